@@ -65,6 +65,40 @@ typedef struct haste_sgd {
     int32_t reserved;    /* must be 0                                                   */
 } haste_sgd_t;
 
+/*
+ * One tensor of the lists that haste_grad_norm and haste_adamw take (HOST array of these structs; the
+ * arrays that they name are on the device).  haste_grad_norm reads grad, n and grad_dtype alone.
+ */
+typedef struct haste_param {
+    void *W;             /* weights [n] in dtype, updated                                         */
+    float *W32;          /* NULL, or the fp32 weights [n] that a bf16 W is the rounded copy of:   */
+                         /* they are read and updated, W is only written                          */
+    const void *grad;    /* gradient [n] in grad_dtype                                            */
+    void *m;             /* first moment [n]: fp32, or E4M3 bytes                                 */
+    void *v;             /* second moment [n]: fp32, or E4M3 bytes that hold its square root      */
+    uint8_t *scale;      /* scales of 8-bit moments [ceil(n / 32)][2] (m's, v's; 2-byte aligned), */
+                         /* else NULL                                                             */
+    int64_t n;           /* values (>= 0; a tensor of none is passed over)                        */
+    float lr_scale;      /* factor of the learning rate for this tensor                           */
+    float weight_decay;  /* decoupled weight decay (0 = none)                                     */
+    int32_t dtype;       /* enum haste_dtype of W                                                 */
+    int32_t grad_dtype;  /* enum haste_dtype of grad                                              */
+    int32_t state_bits;  /* 32 or 8: what m and v are held in                                     */
+    int32_t reserved;    /* must be 0                                                             */
+} haste_param_t;
+
+/* Hyper-parameters of one step of AdamW (see haste_adamw). */
+typedef struct haste_adamw_opts {
+    double lr;              /* learning rate (finite, >= 0)                                       */
+    double beta1, beta2;    /* decay of the moments, in [0, 1)                                    */
+    double eps;             /* added to the root of the second moment (> 0)                       */
+    int64_t step;           /* number of this step, from 1                                        */
+    uint64_t seed;          /* of the random bits that 8-bit moments are rounded with             */
+    const float *lr_dev;       /* NULL, or a DEVICE value that takes the place of lr              */
+    const int64_t *step_dev;   /* NULL, or a DEVICE value (>= 1) that takes the place of step     */
+    const float *grad_scale;   /* NULL, or a DEVICE factor of every gradient (haste_grad_norm's)  */
+} haste_adamw_opts_t;
+
 /* Shape of one sparse tail layer. */
 typedef struct haste_desc {
     int64_t B;      /* batch rows (>= 0)                                         */
@@ -348,6 +382,93 @@ int haste_head_fwd_bce(int64_t B, int64_t F_s, int64_t H, int32_t dtype, const v
 int haste_head_bwd(int64_t B, int64_t F_s, int64_t H, int32_t dtype, const void *X,
                    const void *W_head, const void *dY_h, float *dW_h, float *dX, int beta_dx,
                    void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Layer norm that makes the layer's features from the encoder's output, or any layer norm of rows of F:
+ *   mean[b] = sum_f H[b, f] / F        rstd[b] = 1 / sqrt(sum_f (H[b, f] - mean[b])^2 / F + eps)
+ *   X[b, f] = (H[b, f] - mean[b]) * rstd[b] * weight[f] + bias[f]
+ * H (dtype_h) and X (dtype_x, overwritten) are B rows of F values, ldh and ldx values from one row to the
+ * next (>= F: the first tokens of sequences are rows of one sequence's length times F), aligned to their
+ * elements only.  weight[F], bias[F] fp32 or NULL (ones, zeros).  mean[B], rstd[B] fp32, both or neither
+ * (NULL): what haste_layer_norm_bwd takes.  X may be H where type and stride are the same.
+ * Arithmetic: fp32, the squares around the row's mean; a bf16 X is rounded once.  An infinity or a NaN
+ * makes its own row NaN.  eps >= 0; at 0 a row of equal values is NaN.  F >= 1; B == 0 launches nothing.
+ */
+int haste_layer_norm_fwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t ldh,
+                         const float *weight, const float *bias, float eps, int32_t dtype_x, void *X,
+                         int64_t ldx, float *mean, float *rstd, void *stream);
+
+/*
+ * Backward pass of the layer norm: with xh[b, f] = (H[b, f] - mean[b]) * rstd[b] and
+ * q[b, f] = dX[b, f] * weight[f],
+ *   dH[b, f]   = rstd[b] * (q[b, f] - sum_j q[b, j] / F - xh[b, f] * sum_j q[b, j] xh[b, j] / F)
+ *   dweight[f] = beta * dweight[f] + sum_b dX[b, f] * xh[b, f]
+ *   dbias[f]   = beta * dbias[f] + sum_b dX[b, f]
+ * dX (dtype_dx: the layer's own is fp32) and dH (dtype_h, overwritten) are rows lddx and lddh values apart,
+ * H, ldh, weight, mean and rstd as in the forward call.  dH may be dX where type and stride are the same, and
+ * NULL to skip it; dweight[F] and dbias[F] fp32, each NULL to skip it; beta is 0 (overwrite) or 1
+ * (accumulate).
+ * Sums are fp32; those over rows are formed in parts, in ws, and added in a fixed order.
+ * ws: haste_layer_norm_workspace_bytes(B, F) bytes, where dweight or dbias is asked for.
+ */
+int haste_layer_norm_bwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t ldh,
+                         const float *weight, const float *mean, const float *rstd, int32_t dtype_dx,
+                         const void *dX, int64_t lddx, void *dH, int64_t lddh, float *dweight,
+                         float *dbias, int beta, void *ws, size_t ws_bytes, void *stream);
+
+/* Bytes of workspace haste_layer_norm_bwd needs for dweight and dbias (0 for invalid sizes). */
+size_t haste_layer_norm_workspace_bytes(int64_t B, int64_t F);
+
+/*
+ * Norm of a list of gradients and the factor that clips it to max_norm:
+ *   out[0] = N = sqrt(sum over all tensors and values of grad^2)
+ *   out[1] = N > max_norm ? max_norm / N : 1         (NaN where N is an infinity or a NaN)
+ * out is a DEVICE array of two fp32; out + 1 is what haste_adamw takes as grad_scale.  max_norm > 0, an
+ * infinity to have the norm alone.  Squares and sums are formed in 64 bits, in a fixed order, so that no finite
+ * fp32 gradients overflow; an N beyond fp32 is an infinity in out[0] alone.  No tensors: N is 0.
+ * ws: haste_grad_norm_workspace_bytes(params, n_params) bytes.
+ */
+int haste_grad_norm(const haste_param_t *params, int64_t n_params, float max_norm, float *out, void *ws,
+                    size_t ws_bytes, void *stream);
+
+/* Bytes of workspace haste_grad_norm needs (0 for invalid lists). */
+size_t haste_grad_norm_workspace_bytes(const haste_param_t *params, int64_t n_params);
+
+/*
+ * One step of AdamW (Adam with decoupled weight decay; the paper trains the encoder with Adam, Section 4) over
+ * a list of tensors, in place, in fp32 fused multiply-adds:
+ *   g = grad_scale * grad
+ *   m = beta1 m + (1 - beta1) g                 fma(b1, m, c1 * g)
+ *   v = beta2 v + (1 - beta2) g^2               fma(b2, v, (c2 * g) * g)
+ *   u = (m / (1 - beta1^step)) / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ *   W = W - lr lr_scale (weight_decay W + u)
+ * with b1, b2 the betas and c1, c2 their differences from 1, rounded to fp32.  A bf16 W is rounded to nearest
+ * even: from W32 where there is one, which then carries the step; without one, steps below half of W's last
+ * bit are lost.
+ *
+ * Moments in 8 bits (state_bits 8): blocks of 32 consecutive values, the last one of a tensor maybe shorter,
+ * hold m as E4M3 values and v as those of r = sqrt(v) (OCP FP8: 4 exponent and 3 mantissa bits, 0x7f NaN),
+ * each under a scale of its own per block, a power of two stored as its exponent + 127.  All zero bytes are
+ * moments of zero.  The step uses the moments before they are rounded.  They are then stored so:
+ *   E = max(exponent + 127 of the block's largest finite magnitude, 23);  scale = E - 7, so that the largest
+ *       value is stored in [128, 256);
+ *   a value x is stored as the upper or the lower of the E4M3 values around x / 2^(scale - 127), the upper one
+ *       with a probability of their distance's share (m sign and magnitude): floor(magnitude / spacing +
+ *       d / 65536).  Rounded to nearest, a second moment that moves by a thousandth a step would stay
+ *       where it is; so it moves by the right amount in the mean;
+ *   a root above zero is stored as 2^-9 of the scale at least (else m would later be divided by eps alone);
+ *   an infinity or a NaN becomes a NaN.
+ *   Draws: SplitMix64 as in haste_rewire, with key = out(0) of the stream seeded with seed + step.  Value i of
+ *   tensor k of the list takes the 16 bits from bit 16 (i mod 4) on of out(k 2^40 + floor(i / 4)) of the stream
+ *   seeded with key: d for m, 65535 - d for v.
+ *
+ * Where *grad_scale is an infinity or a NaN, the call changes nothing: a step whose gradients overflowed is
+ * passed over.  lr_dev, step_dev and grad_scale are read when the kernels run, so that a captured graph
+ * follows them.  With step_dev no more than the value is read: the caller counts.
+ * The arrays of the list must not overlap, but that gradients are only read (the same array twice is
+ * refused).  No workspace.  At most 2^16 tensors of up to 2^33 values.
+ */
+int haste_adamw(const haste_param_t *params, int64_t n_params, const haste_adamw_opts_t *opts, void *stream);
 
 /* Bytes of workspace `op` (enum haste_op) needs for this layer; 0 if none.  Never fails; for an
  * invalid descriptor it returns 0 and the call itself reports the error. */

@@ -44,11 +44,25 @@ class haste_group_opts_t(ctypes.Structure):
     _fields_ = [("G", ctypes.c_int64), ("beta", ctypes.c_int64), ("iters", ctypes.c_int64), ("seed", ctypes.c_uint64)]
 
 
+class haste_param_t(ctypes.Structure):
+    _fields_ = [("W", ctypes.c_void_p), ("W32", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("lr_scale", ctypes.c_float), ("weight_decay", ctypes.c_float), ("dtype", ctypes.c_int32),
+                ("grad_dtype", ctypes.c_int32), ("state_bits", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class haste_adamw_opts_t(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", ctypes.c_int64), ("seed", ctypes.c_uint64),
+                ("lr_dev", ctypes.c_void_p), ("step_dev", ctypes.c_void_p), ("grad_scale", ctypes.c_void_p)]
+
+
 def _load() -> ctypes.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"libhaste.so is not built ({LIB_PATH}); run paper_2606_01117_amd.build.build()")
     lib = ctypes.CDLL(LIB_PATH)
-    P, I64, I32, SZ = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t
+    P, I64, I32, SZ, F32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t, ctypes.c_float
+    L = ctypes.POINTER(haste_param_t)
     D = ctypes.POINTER(haste_desc_t)
     sigs = {
         "haste_fwd": [D, P, P, P, P, P, P, SZ, P],
@@ -67,6 +81,10 @@ def _load() -> ctypes.CDLL:
                                 P],
         "haste_head_fwd_bce": [I64, I64, I64, I32, P, P, P, P, I32, P, P],
         "haste_head_bwd": [I64, I64, I64, I32, P, P, P, P, P, ctypes.c_int, P, SZ, P],
+        "haste_layer_norm_fwd": [I64, I64, I32, P, I64, P, P, F32, I32, P, I64, P, P, P],
+        "haste_layer_norm_bwd": [I64, I64, I32, P, I64, P, P, P, I32, P, I64, P, I64, P, P, ctypes.c_int, P, SZ, P],
+        "haste_grad_norm": [L, I64, F32, P, P, SZ, P],
+        "haste_adamw": [L, I64, ctypes.POINTER(haste_adamw_opts_t), P],
         "haste_validate_idx": [D, P, P, P],
         "haste_debug_gather": [D, P, P, I64, I64, P, P],
     }
@@ -80,6 +98,10 @@ def _load() -> ctypes.CDLL:
     lib.haste_head_workspace_bytes.restype = SZ
     lib.haste_group_workspace_bytes.argtypes = [I64, I64, ctypes.POINTER(haste_group_opts_t)]
     lib.haste_group_workspace_bytes.restype = SZ
+    lib.haste_layer_norm_workspace_bytes.argtypes = [I64, I64]
+    lib.haste_layer_norm_workspace_bytes.restype = SZ
+    lib.haste_grad_norm_workspace_bytes.argtypes = [L, I64]
+    lib.haste_grad_norm_workspace_bytes.restype = SZ
     lib.haste_fwd_bce_static_max_bytes.argtypes = []
     lib.haste_fwd_bce_static_max_bytes.restype = SZ
     for name in ("haste_status_str", "haste_last_error", "haste_version"):
@@ -94,6 +116,8 @@ lib = _load()
 EXPORTS = ("haste_fwd", "haste_bwd_w", "haste_bwd_x", "haste_fwd_bce", "haste_fwd_bce_static",
            "haste_fwd_bce_static_max_bytes", "haste_fwd_bce_sgd", "haste_sgd_momentum",
            "haste_rewire", "haste_group_labels", "haste_group_workspace_bytes", "haste_bce_grad", "haste_head_fwd",
+           "haste_layer_norm_fwd", "haste_layer_norm_bwd", "haste_layer_norm_workspace_bytes", "haste_grad_norm",
+           "haste_grad_norm_workspace_bytes", "haste_adamw",
            "haste_head_fwd_bce", "haste_head_bwd", "haste_tail_step", "haste_tail_step_sgd", "haste_workspace_bytes", "haste_head_workspace_bytes", "haste_validate_idx", "haste_debug_gather", "haste_status_str",
            "haste_last_error", "haste_version")
 
@@ -276,6 +300,145 @@ def haste_head_bwd(B, F_s, H, dtype, X, W_head, dY_h, dW_h, dX, beta_dx=0, ws=No
     p, n = _ws(ws)
     _check(lib.haste_head_bwd(B, F_s, H, dtype, _ptr(X), _ptr(W_head), _ptr(dY_h), _ptr(dW_h), _ptr(dX),
                               int(beta_dx), p, n, _stream(stream)))
+
+
+def _rows(t, B, F, dtype, name):
+    """Address and row stride of a [B, F] tensor whose rows may lie apart."""
+    if t is None:
+        return None, F
+    if tuple(t.shape) != (B, F) or t.element_size() != (2 if dtype == HASTE_DTYPE_BF16 else 4):
+        raise ValueError(f"{name} must be [{B}, {F}] of the dtype that the call names, got {tuple(t.shape)} {t.dtype}")
+    if F > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have the values of a row next to each other")
+    if B > 1 and t.stride(0) < F:
+        raise ValueError(f"{name} must have rows that do not overlap")
+    _here(t, name)
+    return t.data_ptr(), t.stride(0) if B > 1 else F
+
+
+def _vec(t, n, name):
+    """Address of a contiguous fp32 vector of n values."""
+    if t is None:
+        return None
+    if t.numel() != n or t.element_size() != 4 or not t.is_floating_point():
+        raise ValueError(f"{name} must be {n} fp32 values, got {tuple(t.shape)} {t.dtype}")
+    _here(t, name)
+    return _ptr(t)
+
+
+def _here(t, name):
+    if t.is_cuda:
+        import torch
+        if t.device.index != torch.cuda.current_device():
+            raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    else:
+        raise ValueError(f"{name} must be on the GPU")
+
+
+def haste_layer_norm_workspace_bytes(B: int, F: int) -> int:
+    return int(lib.haste_layer_norm_workspace_bytes(int(B), int(F)))
+
+
+def haste_layer_norm_fwd(B, F, dtype_h, H, weight, bias, eps, dtype_x, X, mean=None, rstd=None, stream=None):
+    """H and X: [B, F] tensors of dtype_h and dtype_x; their rows may lie apart (a view such as tokens[:, 0])."""
+    (h, ldh), (x, ldx) = _rows(H, B, F, dtype_h, "H"), _rows(X, B, F, dtype_x, "X")
+    _check(lib.haste_layer_norm_fwd(B, F, dtype_h, h, ldh, _vec(weight, F, "weight"), _vec(bias, F, "bias"), eps, dtype_x,
+                                    x, ldx, _vec(mean, B, "mean"), _vec(rstd, B, "rstd"), _stream(stream)))
+
+
+def haste_layer_norm_bwd(B, F, dtype_h, H, weight, mean, rstd, dtype_dx, dX, dH=None, dweight=None, dbias=None, beta=0,
+                         ws=None, stream=None):
+    """dX and dH: [B, F] tensors of dtype_dx and dtype_h, rows apart or not; beta applies to dweight and dbias."""
+    p, n = _ws(ws)
+    (h, ldh), (dx, lddx) = _rows(H, B, F, dtype_h, "H"), _rows(dX, B, F, dtype_dx, "dX")
+    dh, lddh = _rows(dH, B, F, dtype_h, "dH")
+    _check(lib.haste_layer_norm_bwd(B, F, dtype_h, h, ldh, _vec(weight, F, "weight"), _vec(mean, B, "mean"),
+                                    _vec(rstd, B, "rstd"), dtype_dx, dx, lddx, dh, lddh, _vec(dweight, F, "dweight"),
+                                    _vec(dbias, F, "dbias"), int(beta), p, n, _stream(stream)))
+
+
+def _dtype_of(t, name) -> int:
+    import torch
+    if t.dtype == torch.float32:
+        return HASTE_DTYPE_F32
+    if t.dtype == torch.bfloat16:
+        return HASTE_DTYPE_BF16
+    raise ValueError(f"{name} must be torch.float32 or torch.bfloat16, got {t.dtype}")
+
+
+def param(W=None, grad=None, m=None, v=None, scale=None, W32=None, lr_scale=1.0, weight_decay=0.0) -> haste_param_t:
+    """One tensor of a list for haste_grad_norm (which needs grad alone) and haste_adamw.
+
+    W (fp32 or bf16), grad (fp32 or bf16), and the moments m and v: fp32, or of one byte a value (uint8, or
+    float8_e4m3fn) with scale, uint8 [ceil(n / 32), 2].  All contiguous, of n values each.  The entry keeps the
+    tensors alive."""
+    n = (grad if grad is not None else W).numel()
+    p = haste_param_t(n=n, lr_scale=lr_scale, weight_decay=weight_decay, state_bits=32)
+    p.keep = (W, grad, m, v, scale, W32)
+    for t, name in ((W, "W"), (grad, "grad"), (m, "m"), (v, "v"), (W32, "W32")):
+        if t is None:
+            continue
+        if t.numel() != n:
+            raise ValueError(f"{name} has {t.numel()} values, not {n}")
+        _here(t, name)
+        setattr(p, name, _ptr(t))
+    if W is not None:
+        p.dtype = _dtype_of(W, "W")
+    if grad is not None:
+        p.grad_dtype = _dtype_of(grad, "grad")
+    if W32 is not None and _dtype_of(W32, "W32") != HASTE_DTYPE_F32:
+        raise ValueError("W32 must be torch.float32")
+    if m is not None and v is not None:
+        if m.element_size() == 1 and v.element_size() == 1:
+            p.state_bits = 8
+            if scale is None or scale.element_size() != 1 or scale.numel() != 2 * ((n + 31) // 32):
+                raise ValueError(f"8-bit moments of {n} values need scale, uint8 [{(n + 31) // 32}, 2]")
+            _here(scale, "scale")
+            p.scale = _ptr(scale)
+        elif _dtype_of(m, "m") != HASTE_DTYPE_F32 or _dtype_of(v, "v") != HASTE_DTYPE_F32:
+            raise ValueError("m and v must both be torch.float32, or both of one byte a value")
+    return p
+
+
+def param_list(params):
+    """The array of entries that haste_grad_norm and haste_adamw take; made once, it serves every step."""
+    params = list(params)
+    array = (haste_param_t * len(params))(*params)
+    array.keep = [getattr(p, "keep", None) for p in params]
+    return array
+
+
+def adamw_opts(lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, seed=0, lr_dev=None, step_dev=None,
+               grad_scale=None) -> haste_adamw_opts_t:
+    """Options of haste_adamw; the caller sets .step (and .lr) before each call.  lr_dev (fp32), step_dev (int64)
+    and grad_scale (fp32, haste_grad_norm's out[1:]) are GPU tensors of one value, or None."""
+    import torch
+    o = haste_adamw_opts_t(lr=lr, beta1=beta1, beta2=beta2, eps=eps, step=step, seed=seed & ((1 << 64) - 1))
+    o.keep = (lr_dev, step_dev, grad_scale)
+    for t, name, dtype in ((lr_dev, "lr_dev", torch.float32), (step_dev, "step_dev", torch.int64),
+                           (grad_scale, "grad_scale", torch.float32)):
+        if t is None:
+            continue
+        if t.numel() != 1 or t.dtype != dtype:
+            raise ValueError(f"{name} must be one value of {dtype}")
+        _here(t, name)
+        setattr(o, name, t.data_ptr())
+    return o
+
+
+def haste_grad_norm_workspace_bytes(params) -> int:
+    return int(lib.haste_grad_norm_workspace_bytes(params, len(params)))
+
+
+def haste_grad_norm(params, max_norm, out, ws=None, stream=None):
+    """params: a param_list; out: two fp32 values on the GPU, the norm and the factor that clips it to max_norm."""
+    p, n = _ws(ws)
+    _check(lib.haste_grad_norm(params, len(params), max_norm, _vec(out, 2, "out"), p, n, _stream(stream)))
+
+
+def haste_adamw(params, opts, stream=None):
+    """One AdamW step over a param_list, in place."""
+    _check(lib.haste_adamw(params, len(params), ctypes.byref(opts), _stream(stream)))
 
 
 def haste_validate_idx(desc, idx, n_bad_rows, stream=None):

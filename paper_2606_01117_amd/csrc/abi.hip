@@ -649,6 +649,167 @@ int haste_head_bwd(int64_t B, int64_t F_s, int64_t H, int32_t dtype, const void 
     return hip_status(haste::head_bwd(B, F_s, H, dtype, X, W_head, dY_h, dW_h, dX, beta_dx, ws, s), "haste_head_bwd");
 }
 
+static int check_norm(int64_t B, int64_t F, int32_t dtype_a, int32_t dtype_b) {
+    for (int32_t t : {dtype_a, dtype_b})
+        if (t != HASTE_DTYPE_F32 && t != HASTE_DTYPE_BF16) return fail(HASTE_ERR_INVALID, "bad dtype %d", t);
+    if (B < 0 || B > INT32_MAX) return fail(HASTE_ERR_INVALID, "B must be in [0, 2^31)");
+    if (F < 1 || F > INT32_MAX) return fail(HASTE_ERR_INVALID, "F must be in [1, 2^31)");
+    return HASTE_OK;
+}
+
+// rows of F values, ld values apart, aligned to their elements
+static int need_rows(const void *p, int32_t dtype, int64_t F, int64_t ld, const char *name) {
+    if (!p) return fail(HASTE_ERR_INVALID, "%s is NULL", name);
+    if (reinterpret_cast<uintptr_t>(p) % (dtype == HASTE_DTYPE_BF16 ? 2 : 4))
+        return fail(HASTE_ERR_INVALID, "%s is not aligned to its elements", name);
+    if (ld < F) return fail(HASTE_ERR_INVALID, "%s has rows %lld values apart, fewer than F = %lld", name, (long long)ld,
+                            (long long)F);
+    return HASTE_OK;
+}
+
+static int opt_ptr(const void *p, const char *name) { return p ? need_ptr(p, name) : HASTE_OK; }
+
+int haste_layer_norm_fwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t ldh, const float *weight,
+                         const float *bias, float eps, int32_t dtype_x, void *X, int64_t ldx, float *mean, float *rstd,
+                         void *stream) {
+    TRY(check_norm(B, F, dtype_h, dtype_x));
+    if (!(eps >= 0.0f) || isinf(eps)) return fail(HASTE_ERR_INVALID, "eps must be finite and >= 0");
+    if (!mean != !rstd) return fail(HASTE_ERR_INVALID, "mean and rstd are asked for together");
+    if (B == 0) return ok();
+    TRY(need_rows(H, dtype_h, F, ldh, "H"));
+    TRY(need_rows(X, dtype_x, F, ldx, "X"));
+    TRY(opt_ptr(weight, "weight"));
+    TRY(opt_ptr(bias, "bias"));
+    TRY(opt_ptr(mean, "mean"));
+    TRY(opt_ptr(rstd, "rstd"));
+    if (X == H && (dtype_x != dtype_h || ldx != ldh))
+        return fail(HASTE_ERR_INVALID, "X may take H's place only with its type and stride");
+    return hip_status(haste::ln_fwd(B, F, dtype_h, H, ldh, weight, bias, eps, dtype_x, X, ldx, mean, rstd, as_stream(stream)),
+                      "haste_layer_norm_fwd");
+}
+
+size_t haste_layer_norm_workspace_bytes(int64_t B, int64_t F) {
+    return check_norm(B, F, HASTE_DTYPE_F32, HASTE_DTYPE_F32) || B == 0 ? 0 : haste::ln_bwd_ws(B, F);
+}
+
+int haste_layer_norm_bwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t ldh, const float *weight,
+                         const float *mean, const float *rstd, int32_t dtype_dx, const void *dX, int64_t lddx, void *dH,
+                         int64_t lddh, float *dweight, float *dbias, int beta, void *ws, size_t ws_bytes, void *stream) {
+    TRY(check_norm(B, F, dtype_h, dtype_dx));
+    if (beta != 0 && beta != 1) return fail(HASTE_ERR_INVALID, "beta must be 0 or 1");
+    TRY(opt_ptr(dweight, "dweight"));
+    TRY(opt_ptr(dbias, "dbias"));
+    if (dweight && dweight == dbias) return fail(HASTE_ERR_INVALID, "dweight and dbias are the same array");
+    hipStream_t s = as_stream(stream);
+    if (B == 0) {
+        if (dweight && !beta) {
+            const hipError_t e = haste::fill_f32(dweight, F, 0.0f, s);
+            if (e != hipSuccess) return hip_status(e, "haste_layer_norm_bwd");
+        }
+        if (dbias && !beta) return hip_status(haste::fill_f32(dbias, F, 0.0f, s), "haste_layer_norm_bwd");
+        return ok();
+    }
+    if (!dH && !dweight && !dbias) return ok();
+    TRY(need_rows(H, dtype_h, F, ldh, "H"));
+    TRY(need_rows(dX, dtype_dx, F, lddx, "dX"));
+    TRY(opt_ptr(weight, "weight"));
+    TRY(need_ptr(mean, "mean"));
+    TRY(need_ptr(rstd, "rstd"));
+    if (dH) {
+        TRY(need_rows(dH, dtype_h, F, lddh, "dH"));
+        if (dH == dX && (dtype_h != dtype_dx || lddh != lddx))
+            return fail(HASTE_ERR_INVALID, "dH may take dX's place only with its type and stride");
+        if (dH == H) return fail(HASTE_ERR_INVALID, "dH may not take H's place");
+    }
+    if (dweight || dbias) {
+        const size_t need = haste::ln_bwd_ws(B, F);
+        if (!ws || ws_bytes < need)
+            return fail(HASTE_ERR_WORKSPACE, "haste_layer_norm_bwd needs %zu workspace bytes, got %zu", need, ws ? ws_bytes : 0);
+        TRY(need_ptr(ws, "ws"));
+    }
+    return hip_status(haste::ln_bwd(B, F, dtype_h, H, ldh, weight, mean, rstd, dtype_dx, dX, lddx, dH, lddh, dweight, dbias,
+                                    beta, ws, s), "haste_layer_norm_bwd");
+}
+
+// the list as such: number of tensors, their sizes and types of gradient
+static int check_list(const haste_param_t *p, int64_t n) {
+    if (n < 0) return fail(HASTE_ERR_INVALID, "n_params must be >= 0");
+    if (n > haste::kParamsMax) return fail(HASTE_ERR_UNSUPPORTED, "more than 2^16 tensors");
+    if (n > 0 && !p) return fail(HASTE_ERR_INVALID, "params is NULL");
+    for (int64_t k = 0; k < n; ++k) {
+        if (p[k].reserved != 0) return fail(HASTE_ERR_INVALID, "tensor %lld: reserved must be 0", (long long)k);
+        if (p[k].n < 0) return fail(HASTE_ERR_INVALID, "tensor %lld: n must be >= 0", (long long)k);
+        if (p[k].n > haste::kParamValuesMax)
+            return fail(HASTE_ERR_UNSUPPORTED, "tensor %lld: more than 2^33 values", (long long)k);
+        if (p[k].grad_dtype != HASTE_DTYPE_F32 && p[k].grad_dtype != HASTE_DTYPE_BF16)
+            return fail(HASTE_ERR_INVALID, "tensor %lld: bad grad_dtype %d", (long long)k, p[k].grad_dtype);
+    }
+    return HASTE_OK;
+}
+
+// one array of a list's tensor
+static int need_part(const void *p, int64_t k, const char *name) {
+    if (!p) return fail(HASTE_ERR_INVALID, "tensor %lld: %s is NULL", (long long)k, name);
+    if (!aligned16(p)) return fail(HASTE_ERR_INVALID, "tensor %lld: %s is not 16-byte aligned", (long long)k, name);
+    return HASTE_OK;
+}
+
+size_t haste_grad_norm_workspace_bytes(const haste_param_t *params, int64_t n_params) {
+    return check_list(params, n_params) ? 0 : haste::grad_norm_ws(params, n_params);
+}
+
+int haste_grad_norm(const haste_param_t *params, int64_t n_params, float max_norm, float *out, void *ws, size_t ws_bytes,
+                    void *stream) {
+    TRY(check_list(params, n_params));
+    if (!(max_norm > 0.0f)) return fail(HASTE_ERR_INVALID, "max_norm must be > 0");
+    for (int64_t k = 0; k < n_params; ++k)
+        if (params[k].n > 0) TRY(need_part(params[k].grad, k, "grad"));
+    if (!out) return fail(HASTE_ERR_INVALID, "out is NULL");
+    if (reinterpret_cast<uintptr_t>(out) % 4) return fail(HASTE_ERR_INVALID, "out is not 4-byte aligned");
+    const size_t need = haste::grad_norm_ws(params, n_params);
+    if (!ws || ws_bytes < need)
+        return fail(HASTE_ERR_WORKSPACE, "haste_grad_norm needs %zu workspace bytes, got %zu", need, ws ? ws_bytes : 0);
+    TRY(need_ptr(ws, "ws"));
+    return hip_status(haste::grad_norm(params, n_params, max_norm, out, ws, as_stream(stream)), "haste_grad_norm");
+}
+
+int haste_adamw(const haste_param_t *params, int64_t n_params, const haste_adamw_opts_t *opts, void *stream) {
+    TRY(check_list(params, n_params));
+    if (!opts) return fail(HASTE_ERR_INVALID, "opts is NULL");
+    if (!(opts->lr >= 0.0 && opts->lr < 3e38)) return fail(HASTE_ERR_INVALID, "lr must be finite and >= 0");
+    if (!(opts->beta1 >= 0.0 && opts->beta1 < 1.0) || !(opts->beta2 >= 0.0 && opts->beta2 < 1.0))
+        return fail(HASTE_ERR_INVALID, "beta1 and beta2 must be in [0, 1)");
+    if (!((float)opts->eps > 0.0f && opts->eps < 3e38)) return fail(HASTE_ERR_INVALID, "eps must be finite and > 0 (as fp32)");
+    if (!opts->step_dev && opts->step < 1) return fail(HASTE_ERR_INVALID, "step must be >= 1");
+    const uintptr_t odd = reinterpret_cast<uintptr_t>(opts->lr_dev) % 4 | reinterpret_cast<uintptr_t>(opts->step_dev) % 8 |
+                          reinterpret_cast<uintptr_t>(opts->grad_scale) % 4;
+    if (odd) return fail(HASTE_ERR_INVALID, "lr_dev, step_dev and grad_scale must be aligned to their types");
+    for (int64_t k = 0; k < n_params; ++k) {
+        const haste_param_t &p = params[k];
+        if (p.n == 0) continue;
+        if (p.dtype != HASTE_DTYPE_F32 && p.dtype != HASTE_DTYPE_BF16)
+            return fail(HASTE_ERR_INVALID, "tensor %lld: bad dtype %d", (long long)k, p.dtype);
+        if (p.state_bits != 32 && p.state_bits != 8)
+            return fail(HASTE_ERR_INVALID, "tensor %lld: state_bits must be 32 or 8", (long long)k);
+        if (p.W32 && p.dtype != HASTE_DTYPE_BF16)
+            return fail(HASTE_ERR_INVALID, "tensor %lld: W32 goes with bf16 weights", (long long)k);
+        if (!isfinite(p.lr_scale) || !(p.weight_decay >= 0.0f) || isinf(p.weight_decay))
+            return fail(HASTE_ERR_INVALID, "tensor %lld: lr_scale must be finite, weight_decay finite and >= 0", (long long)k);
+        TRY(need_part(p.W, k, "W"));
+        TRY(need_part(p.grad, k, "grad"));
+        TRY(need_part(p.m, k, "m"));
+        TRY(need_part(p.v, k, "v"));
+        if (p.W32) TRY(need_part(p.W32, k, "W32"));
+        if (p.state_bits == 8 && !p.scale) return fail(HASTE_ERR_INVALID, "tensor %lld: scale is NULL", (long long)k);
+        if (p.state_bits == 8 && reinterpret_cast<uintptr_t>(p.scale) % 2)
+            return fail(HASTE_ERR_INVALID, "tensor %lld: scale is not 2-byte aligned", (long long)k);
+    }
+    const int64_t twice = haste::adamw_repeated(params, n_params);
+    if (twice >= 0)
+        return fail(HASTE_ERR_INVALID, "tensor %lld: an array that is updated occurs twice in the list", (long long)twice);
+    return hip_status(haste::adamw(params, n_params, *opts, as_stream(stream)), "haste_adamw");
+}
+
 int haste_validate_idx(const haste_desc_t *d, const int32_t *idx, int32_t *n_bad_rows, void *stream) {
     TRY(check_desc(d));
     if (!n_bad_rows) return fail(HASTE_ERR_INVALID, "n_bad_rows is NULL");

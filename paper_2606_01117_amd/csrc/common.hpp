@@ -325,6 +325,20 @@ hipError_t fwd_bce_sgd_mfma(const TailArgs &a, const void *X, const int32_t *idx
 // momentum step over n weights: m and W_next updated (W_next may alias W)
 hipError_t sgd_momentum(int64_t n, int32_t dtype, const void *W, const float *g, float *m, const haste_sgd_t &opt,
                         void *W_next, hipStream_t s);
+// layer norm of rows; dweight and dbias (either may be NULL) through partial sums in ws (ln_bwd_ws)
+hipError_t ln_fwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t ldh, const float *weight,
+                  const float *bias, float eps, int32_t dtype_x, void *X, int64_t ldx, float *mean, float *rstd,
+                  hipStream_t s);
+size_t ln_bwd_ws(int64_t B, int64_t F);
+hipError_t ln_bwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t ldh, const float *weight,
+                  const float *mean, const float *rstd, int32_t dtype_dx, const void *dX, int64_t lddx, void *dH,
+                  int64_t lddh, float *dweight, float *dbias, int beta, void *ws, hipStream_t s);
+// norm of a list of gradients, and one step of AdamW over a list
+constexpr int64_t kParamsMax = (int64_t)1 << 16, kParamValuesMax = (int64_t)1 << 33;
+size_t grad_norm_ws(const haste_param_t *p, int64_t n);
+hipError_t grad_norm(const haste_param_t *p, int64_t n, float max_norm, float *out, void *ws, hipStream_t s);
+int64_t adamw_repeated(const haste_param_t *p, int64_t n);   // a tensor that names an updated array again, or -1
+hipError_t adamw(const haste_param_t *p, int64_t n, const haste_adamw_opts_t &opt, hipStream_t s);
 // group-shared rewiring (Alg. 3); n_prune >= 1
 bool rewire_supported(const TailArgs &a);
 size_t rewire_ws(const TailArgs &a);
