@@ -91,7 +91,7 @@ typedef struct haste_param {
 typedef struct haste_adamw_opts {
     double lr;              /* learning rate (finite, >= 0)                                       */
     double beta1, beta2;    /* decay of the moments, in [0, 1)                                    */
-    double eps;             /* added to the root of the second moment (> 0)                       */
+    double eps;             /* added to the root of the second moment (>= 1.2e-38)                 */
     int64_t step;           /* number of this step, from 1                                        */
     uint64_t seed;          /* of the random bits that 8-bit moments are rounded with             */
     const float *lr_dev;       /* NULL, or a DEVICE value that takes the place of lr              */

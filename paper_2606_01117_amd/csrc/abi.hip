@@ -779,7 +779,7 @@ int haste_adamw(const haste_param_t *params, int64_t n_params, const haste_adamw
     if (!(opts->lr >= 0.0 && opts->lr < 3e38)) return fail(HASTE_ERR_INVALID, "lr must be finite and >= 0");
     if (!(opts->beta1 >= 0.0 && opts->beta1 < 1.0) || !(opts->beta2 >= 0.0 && opts->beta2 < 1.0))
         return fail(HASTE_ERR_INVALID, "beta1 and beta2 must be in [0, 1)");
-    if (!((float)opts->eps > 0.0f && opts->eps < 3e38)) return fail(HASTE_ERR_INVALID, "eps must be finite and > 0 (as fp32)");
+    if (!(opts->eps >= 1.2e-38 && opts->eps < 3e38)) return fail(HASTE_ERR_INVALID, "eps must be finite and >= 1.2e-38");
     if (!opts->step_dev && opts->step < 1) return fail(HASTE_ERR_INVALID, "step must be >= 1");
     const uintptr_t odd = reinterpret_cast<uintptr_t>(opts->lr_dev) % 4 | reinterpret_cast<uintptr_t>(opts->step_dev) % 8 |
                           reinterpret_cast<uintptr_t>(opts->grad_scale) % 4;
