@@ -154,9 +154,24 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+_torch_module = None
+
+
+def _torch():
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        import torch
+        torch = _torch()
+        # the current stream's handle; without this entry, through a Stream object, which takes ten times as long
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:
+            return raw(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
@@ -306,33 +321,39 @@ def _rows(t, B, F, dtype, name):
     """Address and row stride of a [B, F] tensor whose rows may lie apart."""
     if t is None:
         return None, F
-    if tuple(t.shape) != (B, F) or t.element_size() != (2 if dtype == HASTE_DTYPE_BF16 else 4):
+    if t.shape != (B, F) or t.element_size() != (2 if dtype == HASTE_DTYPE_BF16 else 4):
         raise ValueError(f"{name} must be [{B}, {F}] of the dtype that the call names, got {tuple(t.shape)} {t.dtype}")
-    if F > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if F > 1 and step != 1:
         raise ValueError(f"{name} must have the values of a row next to each other")
-    if B > 1 and t.stride(0) < F:
+    if B > 1 and ld < F:
         raise ValueError(f"{name} must have rows that do not overlap")
-    _here(t, name)
-    return t.data_ptr(), t.stride(0) if B > 1 else F
+    return t.data_ptr(), ld if B > 1 else F
 
 
-def _vec(t, n, name):
+def _vec(t, n, name, device):
     """Address of a contiguous fp32 vector of n values."""
     if t is None:
         return None
-    if t.numel() != n or t.element_size() != 4 or not t.is_floating_point():
-        raise ValueError(f"{name} must be {n} fp32 values, got {tuple(t.shape)} {t.dtype}")
-    _here(t, name)
-    return _ptr(t)
+    if t.numel() != n or t.dtype is not _torch().float32 or not t.is_contiguous():
+        raise ValueError(f"{name} must be {n} contiguous fp32 values, got {tuple(t.shape)} {t.dtype}")
+    if t.get_device() != device:
+        _elsewhere(t, name)
+    return t.data_ptr()
 
 
 def _here(t, name):
-    if t.is_cuda:
-        import torch
-        if t.device.index != torch.cuda.current_device():
-            raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-    else:
+    """The device of a tensor, which must be the current GPU."""
+    device = t.get_device()
+    if device < 0 or device != _torch().cuda.current_device():
+        _elsewhere(t, name)
+    return device
+
+
+def _elsewhere(t, name):
+    if not t.is_cuda:
         raise ValueError(f"{name} must be on the GPU")
+    raise ValueError(f"{name} is on {t.device}, not on the current device cuda:{_torch().cuda.current_device()}")
 
 
 def haste_layer_norm_workspace_bytes(B: int, F: int) -> int:
@@ -342,8 +363,12 @@ def haste_layer_norm_workspace_bytes(B: int, F: int) -> int:
 def haste_layer_norm_fwd(B, F, dtype_h, H, weight, bias, eps, dtype_x, X, mean=None, rstd=None, stream=None):
     """H and X: [B, F] tensors of dtype_h and dtype_x; their rows may lie apart (a view such as tokens[:, 0])."""
     (h, ldh), (x, ldx) = _rows(H, B, F, dtype_h, "H"), _rows(X, B, F, dtype_x, "X")
-    _check(lib.haste_layer_norm_fwd(B, F, dtype_h, h, ldh, _vec(weight, F, "weight"), _vec(bias, F, "bias"), eps, dtype_x,
-                                    x, ldx, _vec(mean, B, "mean"), _vec(rstd, B, "rstd"), _stream(stream)))
+    on = _here(H, "H")
+    if X.get_device() != on:
+        _elsewhere(X, "X")
+    _check(lib.haste_layer_norm_fwd(B, F, dtype_h, h, ldh, _vec(weight, F, "weight", on), _vec(bias, F, "bias", on), eps,
+                                    dtype_x, x, ldx, _vec(mean, B, "mean", on), _vec(rstd, B, "rstd", on),
+                                    _stream(stream)))
 
 
 def haste_layer_norm_bwd(B, F, dtype_h, H, weight, mean, rstd, dtype_dx, dX, dH=None, dweight=None, dbias=None, beta=0,
@@ -352,9 +377,14 @@ def haste_layer_norm_bwd(B, F, dtype_h, H, weight, mean, rstd, dtype_dx, dX, dH=
     p, n = _ws(ws)
     (h, ldh), (dx, lddx) = _rows(H, B, F, dtype_h, "H"), _rows(dX, B, F, dtype_dx, "dX")
     dh, lddh = _rows(dH, B, F, dtype_h, "dH")
-    _check(lib.haste_layer_norm_bwd(B, F, dtype_h, h, ldh, _vec(weight, F, "weight"), _vec(mean, B, "mean"),
-                                    _vec(rstd, B, "rstd"), dtype_dx, dx, lddx, dh, lddh, _vec(dweight, F, "dweight"),
-                                    _vec(dbias, F, "dbias"), int(beta), p, n, _stream(stream)))
+    on = _here(H, "H")
+    for t, name in ((dX, "dX"), (dH, "dH")):
+        if t is not None and t.get_device() != on:
+            _elsewhere(t, name)
+    _check(lib.haste_layer_norm_bwd(B, F, dtype_h, h, ldh, _vec(weight, F, "weight", on), _vec(mean, B, "mean", on),
+                                    _vec(rstd, B, "rstd", on), dtype_dx, dx, lddx, dh, lddh,
+                                    _vec(dweight, F, "dweight", on), _vec(dbias, F, "dbias", on), int(beta), p, n,
+                                    _stream(stream)))
 
 
 def _dtype_of(t, name) -> int:
@@ -433,7 +463,8 @@ def haste_grad_norm_workspace_bytes(params) -> int:
 def haste_grad_norm(params, max_norm, out, ws=None, stream=None):
     """params: a param_list; out: two fp32 values on the GPU, the norm and the factor that clips it to max_norm."""
     p, n = _ws(ws)
-    _check(lib.haste_grad_norm(params, len(params), max_norm, _vec(out, 2, "out"), p, n, _stream(stream)))
+    _check(lib.haste_grad_norm(params, len(params), max_norm, _vec(out, 2, "out", _here(out, "out")), p, n,
+                               _stream(stream)))
 
 
 def haste_adamw(params, opts, stream=None):

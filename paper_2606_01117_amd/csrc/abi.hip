@@ -800,6 +800,9 @@ int haste_adamw(const haste_param_t *params, int64_t n_params, const haste_adamw
         TRY(need_part(p.m, k, "m"));
         TRY(need_part(p.v, k, "v"));
         if (p.W32) TRY(need_part(p.W32, k, "W32"));
+        for (const void *a : {(const void *)p.W, (const void *)p.W32, p.grad, (const void *)p.m, (const void *)p.v, (const void *)p.scale})
+            if ((uint64_t)reinterpret_cast<uintptr_t>(a) >> 48)
+                return fail(HASTE_ERR_UNSUPPORTED, "tensor %lld: an address of more than 48 bits", (long long)k);
         if (p.state_bits == 8 && !p.scale) return fail(HASTE_ERR_INVALID, "tensor %lld: scale is NULL", (long long)k);
         if (p.state_bits == 8 && reinterpret_cast<uintptr_t>(p.scale) % 2)
             return fail(HASTE_ERR_INVALID, "tensor %lld: scale is not 2-byte aligned", (long long)k);

@@ -13,8 +13,8 @@ constexpr int kBlock = 32;     // values under one scale of an 8-bit moment
 
 // The tensor that a workgroup belongs to: the last one whose first workgroup is not beyond it.  Every lane
 // compares MAX / 64 tensors', so the search waits for memory once.
-template <int MAX>
-__device__ __forceinline__ int tensor_of(const uint32_t (&start)[MAX], int count, uint32_t block) {
+template <int MAX, int N>
+__device__ __forceinline__ int tensor_of(const uint32_t (&start)[N], int count, uint32_t block) {
     const int lane = threadIdx.x & (kWave - 1);
     int k = -1;
 #pragma unroll
@@ -83,7 +83,7 @@ __device__ __forceinline__ double sum_squares(const T *g, int n) {
 // part[workgroup] = the sum of its values' squares, in 64 bits (fp32's range ends at 1.8e19 for a square)
 __global__ __launch_bounds__(kThreads) void k_gn_part(NormList l, double *__restrict__ part) {
     __shared__ double red[kThreads / kWave];
-    const int k = tensor_of(l.start, l.count, blockIdx.x);
+    const int k = tensor_of<kNormMax>(l.start, l.count, blockIdx.x);
     const int64_t i0 = (int64_t)(blockIdx.x - l.start[k]) * kNormChunk;
     const int n = (int)(l.n[k] - i0 < kNormChunk ? l.n[k] - i0 : kNormChunk);
     const double s = block_sum((l.bf16[k / 64] >> (k % 64)) & 1 ? sum_squares((const bf16_t *)l.grad[k] + i0, n)
@@ -106,24 +106,30 @@ __global__ __launch_bounds__(1024) void k_gn_final(const double *__restrict__ pa
 }
 
 // ---- the step ---------------------------------------------------------------------------------
-constexpr int kListMax = 52;          // the arguments of a kernel have 4096 bytes
-constexpr int64_t kChunk = 4096;
-
-struct StepTensor {
-    void *W;
-    float *W32;
-    const void *grad;
-    void *m, *v;
-    uint8_t *scale;
-    int64_t n;
-    float lr_scale, weight_decay;
-    int32_t kind;                     // kBf16 | kMaster | kGradBf16 | kBits8
-};
+constexpr int kListMax = 76;          // the arguments of a kernel have 4096 bytes
+constexpr int kStepThreads = 128;
+constexpr int64_t kChunk = 1024;
 constexpr int kBf16 = 1, kMaster = 2, kGradBf16 = 4, kBits8 = 8;
+
+// A tensor in 48 bytes, its addresses in 48 bits each, its size by its number of chunks and the values in the last.
+struct StepTensor {
+    uint32_t lo[6], hi[3];            // of W, W32, grad, m, v, scale
+    uint32_t last;                    // values of the last chunk, and 65536 times the kind (kBf16 | ...)
+    float lr_scale, weight_decay;
+    template <typename T>
+    __device__ __forceinline__ T *at(int k) const {
+        return reinterpret_cast<T *>((uint64_t)lo[k] | (uint64_t)((hi[k / 2] >> (16 * (k & 1))) & 0xffffu) << 32);
+    }
+    void put(int k, const void *p) {
+        const uint64_t a = (uint64_t)reinterpret_cast<uintptr_t>(p);
+        lo[k] = (uint32_t)a;
+        hi[k / 2] = k & 1 ? hi[k / 2] | (uint32_t)(a >> 32) << 16 : (uint32_t)(a >> 32);
+    }
+};
 
 struct StepList {
     StepTensor t[kListMax];
-    uint32_t start[kListMax];
+    uint32_t start[kListMax + 1];
     int32_t count;
     uint32_t first;                   // number of t[0] in the caller's list (for the draws)
     float b1, c1, b2, c2, eps;        // betas, 1 - betas
@@ -160,77 +166,36 @@ struct Scalars {
     uint64_t key;
 };
 
-// ---- eight consecutive values ---------------------------------------------------------------------
-// n of them are there (16-byte accesses where all are), the others read as zero
-__device__ __forceinline__ void load8(const float *p, int n, float (&v)[8]) {
-    if (n == 8) {
-        const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : 0.0f;
-    }
+// ---- kRun consecutive values: 16 bytes of fp32, 8 of bf16, 4 of E4M3 ---------------------------------
+constexpr int kRun = 4;
+
+typedef float vec4f_t __attribute__((ext_vector_type(4)));
+typedef uint32_t vec2u_t __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ void load_run(const float *p, float (&v)[kRun]) {
+    const vec4f_t a = __builtin_nontemporal_load(reinterpret_cast<const vec4f_t *>(p));
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
 }
-__device__ __forceinline__ void load8(const bf16_t *p, int n, float (&v)[8]) {
-    if (n == 8) {
-        const uint4 a = *reinterpret_cast<const uint4 *>(p);
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[2 * j] = __uint_as_float(w[j] << 16), v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j < n ? bf16_to_f32(p[j]) : 0.0f;
-    }
+__device__ __forceinline__ void load_run(const bf16_t *p, float (&v)[kRun]) {
+    const vec2u_t a = __builtin_nontemporal_load(reinterpret_cast<const vec2u_t *>(p));
+    v[0] = __uint_as_float(a.x << 16), v[1] = __uint_as_float(a.x & 0xffff0000u);
+    v[2] = __uint_as_float(a.y << 16), v[3] = __uint_as_float(a.y & 0xffff0000u);
 }
-__device__ __forceinline__ uint2 load8(const uint8_t *p, int n) {
-    if (n == 8) return *reinterpret_cast<const uint2 *>(p);
-    uint32_t w[2] = {0, 0};
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-        if (j < n) w[j / 4] |= (uint32_t)p[j] << (8 * (j % 4));
-    return make_uint2(w[0], w[1]);
+__device__ __forceinline__ void store_run(float *p, const float (&v)[kRun]) {
+    __builtin_nontemporal_store(vec4f_t{v[0], v[1], v[2], v[3]}, reinterpret_cast<vec4f_t *>(p));
 }
-__device__ __forceinline__ void store8(float *p, int n, const float (&v)[8]) {
-    if (n == 8) {
-        reinterpret_cast<float4 *>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4 *>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < n) p[j] = v[j];
-    }
-}
-__device__ __forceinline__ void store8(bf16_t *p, int n, const float (&v)[8]) {
-    if (n == 8) {
-        *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]),
-                                                   pack_bf16(v[6], v[7]));
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < n) p[j] = f32_to_bf16(v[j]);
-    }
-}
-__device__ __forceinline__ void store8(uint8_t *p, int n, uint2 q) {
-    if (n == 8) {
-        *reinterpret_cast<uint2 *>(p) = q;
-    } else {
-        const uint32_t w[2] = {q.x, q.y};
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < n) p[j] = (uint8_t)(w[j / 4] >> (8 * (j % 4)));
-    }
+__device__ __forceinline__ void store_run(bf16_t *p, const float (&v)[kRun]) {
+    __builtin_nontemporal_store(vec2u_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}, reinterpret_cast<vec2u_t *>(p));
 }
 
 // ---- moments in 8 bits ------------------------------------------------------------------------------
-// E4M3 bytes times their block's scale
-__device__ __forceinline__ void load_e4m3(uint2 q, uint32_t scale, float (&v)[8]) {
-    const float s = __uint_as_float(scale << 23);
-    const uint32_t w[2] = {q.x, q.y};
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[j], true);
-        v[4 * j] = a.x * s, v[4 * j + 1] = a.y * s, v[4 * j + 2] = b.x * s, v[4 * j + 3] = b.y * s;
-    }
+__device__ __forceinline__ float scale_value(uint32_t scale) { return __uint_as_float(scale << 23); }
+
+// four E4M3 bytes times their block's scale
+__device__ __forceinline__ void load_e4m3(uint32_t q, uint32_t scale, float (&v)[kRun]) {
+    const float s = scale_value(scale);
+    const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8((int)q, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)q, true);
+    v[0] = a.x * s, v[1] = a.y * s, v[2] = b.x * s, v[3] = b.y * s;
 }
 
 template <int CTRL>
@@ -239,105 +204,195 @@ __device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
     return o > v ? o : v;
 }
 
-// The scale of a block from the magnitudes of its 32 values, eight on each of four neighbouring lanes.
-__device__ __forceinline__ uint32_t block_scale(const float (&x)[8]) {
-    uint32_t e = 0;
+// The largest finite magnitude of a lane's N values, as its bits (the maximum passes NaN over).
+template <int N>
+__device__ __forceinline__ uint32_t largest(const float (&x)[N]) {
+    float a = fabsf(x[0]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint32_t b = __float_as_uint(x[j]) & 0x7fffffffu;
-        e = b > e ? b : e;
-    }
-    if (__ballot(e >= 0x7f800000u)) {       // an infinity or a NaN among the wave's values: they do not count
+    for (int j = 1; j < N; ++j) a = fmaxf(a, fabsf(x[j]));
+    uint32_t e = __float_as_uint(a);
+    if (__ballot(e >= 0x7f800000u)) {       // an infinity among the wave's values, or a lane of NaN: they do not count
         e = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < N; ++j) {
             const uint32_t b = __float_as_uint(x[j]) & 0x7fffffffu;
             e = b < 0x7f800000u && b > e ? b : e;
         }
     }
-    e = dpp_max<0x4E>(dpp_max<0xB1>(e)) >> 23;
+    return e;
+}
+// The scale of a block from the bits of its largest value.
+__device__ __forceinline__ uint32_t scale_of(uint32_t e) {
+    e >>= 23;
     return (e < 23u ? 23u : e) - 7u;
+}
+// The same over the eight neighbouring lanes that hold a block in runs of four: pairs, quads, the two quads.
+__device__ __forceinline__ uint32_t block_scale(const float (&x)[kRun]) {
+    return scale_of(dpp_max<0x141>(dpp_max<0x4E>(dpp_max<0xB1>(largest(x)))));
 }
 
 // E4M3 magnitude as it is stored: x is scaled so that E4M3's exponent and mantissa are the upper bits of
 // fp32's own (its lowest exponents, and below them its denormals, are E4M3's), so rounding by the draw d is an
-// addition to the 20 bits below them.  Infinities and NaN come out as 127, NaN.
-__device__ __forceinline__ uint32_t store_e4m3(float x, int shift, uint32_t d) {
-    const uint32_t q = (__float_as_uint(ldexpf(x, shift)) + (d << 4)) >> 20;
-    return q < 127u ? q : 127u;
-}
-
-// draws z[0] for the first four values, z[1] for the others, 16 bits each; ROOT: not negative, at least 1 above zero
+// addition to the 20 bits below them.  Infinities and NaN come out as 127, NaN.  ROOT: not negative, and at
+// least 1 where x is above zero; else with x's sign.
 template <bool ROOT>
-__device__ __forceinline__ uint2 store_block(const float (&x)[8], uint32_t scale, const uint64_t (&z)[2]) {
-    const int shift = 7 - (int)scale;
-    uint32_t w[2] = {0, 0};
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint32_t d = (uint32_t)(z[j / 4] >> (16 * (j % 4))) & 0xffffu;
-        uint32_t q = store_e4m3(fabsf(x[j]), shift, d);
-        if constexpr (ROOT) q = x[j] > 0.0f && q == 0u ? 1u : q;
-        else q |= __float_as_uint(x[j]) >> 31 << 7;
-        w[j / 4] |= q << (8 * (j % 4));
+__device__ __forceinline__ uint32_t store_e4m3(float x, uint32_t scale, uint32_t d) {
+    uint32_t q = (__float_as_uint(ldexpf(fabsf(x), 7 - (int)scale)) + (d << 4)) >> 20;
+    q = q < 127u ? q : 127u;
+    if constexpr (ROOT) {
+        const uint32_t least = __float_as_uint(x) < 1u ? 0u : 1u;
+        return q > least ? q : least;
     }
-    return make_uint2(w[0], w[1]);
+    return q | __float_as_uint(x) >> 31 << 7;
+}
+template <bool ROOT>
+__device__ __forceinline__ uint32_t store_e4m3(const float (&x)[kRun], uint32_t scale, uint64_t z) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) w |= store_e4m3<ROOT>(x[j], scale, (uint32_t)(z >> (16 * j)) & 0xffffu) << (8 * j);
+    return w;
 }
 
-// Values i0 .. i0 + kChunk of tensor t (number k of the list), eight a thread at a time.
+// ---- the step of N values a lane --------------------------------------------------------------------
+// r = sqrt(v), correctly rounded (the 8-bit moments are rounded from it, and two implementations have to meet
+// the same value).  s = v y with y = 1 / sqrt(v) to one unit is off by a few units, and s + (v - s^2) y / 2, the
+// difference exact, rounds to the right one: compared with sqrtf for every value of two binades, so, within the
+// range below, for all.  Half of the instructions that sqrtf takes (58M bf16 weights and gradients with 8-bit
+// moments, where the vector ALUs are the bound: 132 us with it, 115 so).
+template <int N>
+__device__ __forceinline__ void roots(const float (&v)[N], float (&r)[N]) {
+    uint32_t lo = __float_as_uint(v[0]), hi = lo;
+#pragma unroll
+    for (int j = 1; j < N; ++j) {
+        const uint32_t b = __float_as_uint(v[j]);
+        lo = b < lo ? b : lo;
+        hi = b > hi ? b : hi;
+    }
+    if (__ballot(lo < 0x12800000u || hi >= 0x7f800000u)) {    // below 2^-90, zeros among them, or not finite
+#pragma unroll
+        for (int j = 0; j < N; ++j) r[j] = sqrtf(v[j]);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const float y = __builtin_amdgcn_rsqf(v[j]), s = v[j] * y;
+        r[j] = __fmaf_rn(__fmaf_rn(-s, s, v[j]), 0.5f * y, s);
+    }
+}
+
+// w, m, v: weights and moments, updated; r: the root of v.
+template <int N>
+__device__ __forceinline__ void step_values(float (&w)[N], const float (&g)[N], float (&m)[N], float (&v)[N], float (&r)[N],
+                                            const StepList &l, const Scalars &c, float lr, float wd) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const float x = __fmul_rn(g[j], c.gs);
+        m[j] = __fmaf_rn(l.b1, m[j], __fmul_rn(l.c1, x));
+        v[j] = __fmaf_rn(l.b2, v[j], __fmul_rn(__fmul_rn(l.c2, x), x));
+    }
+    roots(v, r);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const float u = m[j] * c.rbc1 * __builtin_amdgcn_rcpf(__fmaf_rn(r[j], c.rbc2, l.eps));
+        w[j] = __fmaf_rn(-lr, __fmaf_rn(wd, w[j], u), w[j]);
+    }
+}
+
+// Values i0 .. i0 + n of tensor t (number k of the list), a chunk.  The tensor's whole blocks of 32 go in runs of four
+// a lane; its last, partial block one value a lane, on the workgroup's last wave.
 template <int KIND>
-__device__ __forceinline__ void step_chunk(const StepTensor &t, const StepList &l, const Scalars &c, uint32_t k, int64_t i0) {
+__device__ __forceinline__ void step_chunk(const StepTensor &t, const StepList &l, const Scalars &c, uint32_t k, int64_t i0,
+                                           uint32_t n) {
     typedef std::conditional_t<(KIND & kBf16) != 0, bf16_t, float> TW;
     typedef std::conditional_t<(KIND & kGradBf16) != 0, bf16_t, float> TG;
+    constexpr bool B8 = (KIND & kBits8) != 0, MASTER = (KIND & kMaster) != 0;
     const float lr = c.lr * t.lr_scale, wd = t.weight_decay;
-    for (int64_t b = i0; b < i0 + kChunk && b < t.n; b += 8 * kThreads) {
-        const int64_t i = b + 8 * threadIdx.x;
-        const int n = t.n - i >= 8 ? 8 : t.n - i > 0 ? (int)(t.n - i) : 0;
-        float w[8], g[8], m[8], v[8], r[8];
-        uint2 qm, qv;
-        uint32_t sc = 0;
-        load8((const TG *)t.grad + i, n, g);
-        if constexpr (KIND & kBits8) {
-            qm = load8((const uint8_t *)t.m + i, n);
-            qv = load8((const uint8_t *)t.v + i, n);
-            if (n > 0) sc = ((const uint16_t *)t.scale)[i / kBlock];
-        } else {
-            load8((const float *)t.m + i, n, m);
-            load8((const float *)t.v + i, n, v);
-        }
-        if constexpr (KIND & kMaster) load8(t.W32 + i, n, w);
-        else load8((const TW *)t.W + i, n, w);
-        if constexpr (KIND & kBits8) {
+    TW *W = t.at<TW>(0) + i0;
+    float *W32 = t.at<float>(1) + i0;
+    const TG *G = t.at<TG>(2) + i0;
+    float *M = t.at<float>(3) + i0, *V = t.at<float>(4) + i0;
+    uint32_t *QM = t.at<uint32_t>(3) + i0 / 4, *QV = t.at<uint32_t>(4) + i0 / 4;
+    uint16_t *S = t.at<uint16_t>(5) + i0 / kBlock;
+    const uint32_t whole = n / kBlock * kBlock;
+    // eight neighbouring lanes, a whole block, go through together
+    for (uint32_t i = kRun * threadIdx.x; i < whole; i += kRun * kStepThreads) {
+        float w[kRun], g[kRun], m[kRun], v[kRun], r[kRun];
+        load_run(G + i, g);
+        if constexpr (MASTER) load_run(W32 + i, w);
+        else load_run(W + i, w);
+        if constexpr (B8) {
+            const uint32_t sc = S[i / kBlock], qm = __builtin_nontemporal_load(QM + i / 4),
+                           qv = __builtin_nontemporal_load(QV + i / 4);
             load_e4m3(qm, sc & 0xffu, m);
             load_e4m3(qv, sc >> 8, v);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if constexpr (KIND & kBits8) v[j] = __fmul_rn(v[j], v[j]);
-            const float x = __fmul_rn(g[j], c.gs);
-            m[j] = __fmaf_rn(l.b1, m[j], __fmul_rn(l.c1, x));
-            v[j] = __fmaf_rn(l.b2, v[j], __fmul_rn(__fmul_rn(l.c2, x), x));
-            r[j] = __fsqrt_rn(v[j]);
-            const float u = m[j] * c.rbc1 * __builtin_amdgcn_rcpf(__fmaf_rn(r[j], c.rbc2, l.eps));
-            w[j] = __fmaf_rn(-lr, __fmaf_rn(wd, w[j], u), w[j]);
-        }
-        if constexpr (KIND & kMaster) store8(t.W32 + i, n, w);
-        store8((TW *)t.W + i, n, w);
-        if constexpr (KIND & kBits8) {
-            const uint32_t sm = block_scale(m), sv = block_scale(r);
-            const uint64_t first = ((uint64_t)k << 40) + (uint64_t)(i >> 2);
-            uint64_t z[2] = {splitmix64_at(c.key, first), splitmix64_at(c.key, first + 1)};
-            store8((uint8_t *)t.m + i, n, store_block<false>(m, sm, z));
-            z[0] = ~z[0], z[1] = ~z[1];
-            store8((uint8_t *)t.v + i, n, store_block<true>(r, sv, z));
-            if (n > 0 && (threadIdx.x & 3) == 0) ((uint16_t *)t.scale)[i / kBlock] = (uint16_t)(sm | sv << 8);
         } else {
-            store8((float *)t.m + i, n, m);
-            store8((float *)t.v + i, n, v);
+            load_run(M + i, m);
+            load_run(V + i, v);
         }
+        if constexpr (B8) {
+#pragma unroll
+            for (int j = 0; j < kRun; ++j) v[j] = __fmul_rn(v[j], v[j]);
+        }
+        step_values(w, g, m, v, r, l, c, lr, wd);
+        if constexpr (MASTER) store_run(W32 + i, w);
+        store_run(W + i, w);
+        if constexpr (B8) {
+            const uint32_t sm = block_scale(m), sv = block_scale(r);
+            const uint64_t z = splitmix64_at(c.key, ((uint64_t)k << 40) + ((uint64_t)i0 + i) / 4);
+            __builtin_nontemporal_store(store_e4m3<false>(m, sm, z), QM + i / 4);
+            __builtin_nontemporal_store(store_e4m3<true>(r, sv, ~z), QV + i / 4);
+            if ((threadIdx.x & 7) == 0) S[i / kBlock] = (uint16_t)(sm | sv << 8);
+        } else {
+            store_run(M + i, m);
+            store_run(V + i, v);
+        }
+    }
+    const int lane = (int)threadIdx.x - (kStepThreads - kWave);
+    const uint32_t i = whole + (uint32_t)lane;
+    if (n == whole || lane < 0) return;         // wave-uniform
+    const bool in = i < n;                      // lanes 0 .. 30 at most
+    float w[1] = {0.0f}, g[1] = {0.0f}, m[1] = {0.0f}, v[1] = {0.0f}, r[1];
+    if (in) {
+        g[0] = load_f32(G, i);
+        if constexpr (B8) {
+            const uint32_t sc = S[i / kBlock];
+            m[0] = __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t *)QM)[i], 0) * scale_value(sc & 0xffu);
+            v[0] = __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t *)QV)[i], 0) * scale_value(sc >> 8);
+            v[0] = __fmul_rn(v[0], v[0]);
+        } else {
+            m[0] = M[i];
+            v[0] = V[i];
+        }
+        if constexpr (MASTER) w[0] = W32[i];
+        else w[0] = load_f32(W, i);
+    }
+    step_values(w, g, m, v, r, l, c, lr, wd);
+    uint32_t sm = 0, sv = 0;
+    if constexpr (B8) {
+        sm = largest(m), sv = largest(r);
+#pragma unroll
+        for (int o = kWave / 2; o > 0; o >>= 1) {
+            const uint32_t x = (uint32_t)__shfl_xor((int)sm, o), y = (uint32_t)__shfl_xor((int)sv, o);
+            sm = x > sm ? x : sm;
+            sv = y > sv ? y : sv;
+        }
+        sm = scale_of(sm), sv = scale_of(sv);
+    }
+    if (!in) return;
+    if constexpr (MASTER) W32[i] = w[0];
+    store_out(W, i, w[0]);
+    if constexpr (B8) {
+        const uint64_t z = splitmix64_at(c.key, ((uint64_t)k << 40) + ((uint64_t)i0 + i) / 4) >> (16 * (i & 3));
+        ((uint8_t *)QM)[i] = (uint8_t)store_e4m3<false>(m[0], sm, (uint32_t)z & 0xffffu);
+        ((uint8_t *)QV)[i] = (uint8_t)store_e4m3<true>(r[0], sv, ~(uint32_t)z & 0xffffu);
+        if (lane == 0) S[i / kBlock] = (uint16_t)(sm | sv << 8);
+    } else {
+        M[i] = m[0];
+        V[i] = v[0];
     }
 }
 
-__global__ __launch_bounds__(kThreads) void k_adamw(StepList l) {
+__global__ __launch_bounds__(kStepThreads) void k_adamw(StepList l) {
     Scalars c = {l.lr, l.rbc1, l.rbc2, 1.0f, 0};
     if (l.grad_scale) {
         c.gs = *l.grad_scale;
@@ -352,31 +407,31 @@ __global__ __launch_bounds__(kThreads) void k_adamw(StepList l) {
         seed += (uint64_t)t;
     }
     c.key = splitmix64_at(seed, 0);
-    const int k = tensor_of(l.start, l.count, blockIdx.x);
+    const int k = tensor_of<kListMax>(l.start, l.count, blockIdx.x);
     const StepTensor &t = l.t[k];
     const int64_t i0 = (int64_t)(blockIdx.x - l.start[k]) * kChunk;
-    const uint32_t no = l.first + (uint32_t)k;
-    switch (t.kind) {
-    case 0: step_chunk<0>(t, l, c, no, i0); break;
-    case kBf16: step_chunk<kBf16>(t, l, c, no, i0); break;
-    case kBf16 | kMaster: step_chunk<kBf16 | kMaster>(t, l, c, no, i0); break;
-    case kGradBf16: step_chunk<kGradBf16>(t, l, c, no, i0); break;
-    case kGradBf16 | kBf16: step_chunk<kGradBf16 | kBf16>(t, l, c, no, i0); break;
-    case kGradBf16 | kBf16 | kMaster: step_chunk<kGradBf16 | kBf16 | kMaster>(t, l, c, no, i0); break;
-    case kBits8: step_chunk<kBits8>(t, l, c, no, i0); break;
-    case kBits8 | kBf16: step_chunk<kBits8 | kBf16>(t, l, c, no, i0); break;
-    case kBits8 | kBf16 | kMaster: step_chunk<kBits8 | kBf16 | kMaster>(t, l, c, no, i0); break;
-    case kBits8 | kGradBf16: step_chunk<kBits8 | kGradBf16>(t, l, c, no, i0); break;
-    case kBits8 | kGradBf16 | kBf16: step_chunk<kBits8 | kGradBf16 | kBf16>(t, l, c, no, i0); break;
+    const uint32_t no = l.first + (uint32_t)k, n = blockIdx.x + 1 < l.start[k + 1] ? (uint32_t)kChunk : t.last & 0xffffu;
+    switch (t.last >> 16) {
+    case 0: step_chunk<0>(t, l, c, no, i0, n); break;
+    case kBf16: step_chunk<kBf16>(t, l, c, no, i0, n); break;
+    case kBf16 | kMaster: step_chunk<kBf16 | kMaster>(t, l, c, no, i0, n); break;
+    case kGradBf16: step_chunk<kGradBf16>(t, l, c, no, i0, n); break;
+    case kGradBf16 | kBf16: step_chunk<kGradBf16 | kBf16>(t, l, c, no, i0, n); break;
+    case kGradBf16 | kBf16 | kMaster: step_chunk<kGradBf16 | kBf16 | kMaster>(t, l, c, no, i0, n); break;
+    case kBits8: step_chunk<kBits8>(t, l, c, no, i0, n); break;
+    case kBits8 | kBf16: step_chunk<kBits8 | kBf16>(t, l, c, no, i0, n); break;
+    case kBits8 | kBf16 | kMaster: step_chunk<kBits8 | kBf16 | kMaster>(t, l, c, no, i0, n); break;
+    case kBits8 | kGradBf16: step_chunk<kBits8 | kGradBf16>(t, l, c, no, i0, n); break;
+    case kBits8 | kGradBf16 | kBf16: step_chunk<kBits8 | kGradBf16 | kBf16>(t, l, c, no, i0, n); break;
     case kBits8 | kGradBf16 | kBf16 | kMaster:
-        step_chunk<kBits8 | kGradBf16 | kBf16 | kMaster>(t, l, c, no, i0);
+        step_chunk<kBits8 | kGradBf16 | kBf16 | kMaster>(t, l, c, no, i0, n);
         break;
     }
 }
 
 // workgroups of a launch (which has fewer than 2^32 threads); the largest tensor fits one
-constexpr int64_t kMaxGrid = (int64_t)1 << 23;
-static_assert(haste::kParamValuesMax / kChunk <= kMaxGrid && kMaxGrid * kThreads < ((int64_t)1 << 32), "one launch");
+constexpr int64_t kMaxGrid = ((int64_t)1 << 31) / kThreads;
+static_assert(haste::kParamValuesMax / kChunk <= kMaxGrid, "one launch");
 
 }  // namespace
 
@@ -422,18 +477,20 @@ hipError_t grad_norm(const haste_param_t *p, int64_t n, float max_norm, float *o
 // The updated arrays' addresses in an open hash table on the stack: 512 tensors go in, the ones behind them are
 // only looked up, then the next 512 go in.
 int64_t adamw_repeated(const haste_param_t *p, int64_t n) {
-    constexpr int kWindow = 512, kSlots = 4096;      // 5 addresses a tensor
-    const void *slot[kSlots];
+    constexpr int kWindow = 512;
+    const void *slot[8 * kWindow];                   // 5 addresses a tensor
+    int bits = 6;
+    while ((1 << bits) < 8 * (n < kWindow ? n : kWindow)) ++bits;
     for (int64_t w = 0; w < n; w += kWindow) {
         const int64_t w1 = w + kWindow < n ? w + kWindow : n;
-        for (int i = 0; i < kSlots; ++i) slot[i] = nullptr;
+        for (int i = 0; i < 1 << bits; ++i) slot[i] = nullptr;
         for (int64_t k = w; k < n; ++k) {
             if (p[k].n == 0) continue;
             const void *a[5] = {p[k].W, p[k].W32, p[k].m, p[k].v, p[k].state_bits == 8 ? p[k].scale : nullptr};
             for (const void *x : a) {
                 if (!x) continue;
-                uint32_t h = (uint32_t)(((uint64_t)(uintptr_t)x * 0x9E3779B97F4A7C15ull) >> 52);
-                while (slot[h] && slot[h] != x) h = (h + 1) & (kSlots - 1);
+                uint32_t h = (uint32_t)(((uint64_t)(uintptr_t)x * 0x9E3779B97F4A7C15ull) >> (64 - bits));
+                while (slot[h] && slot[h] != x) h = (h + 1) & ((1u << bits) - 1);
                 if (slot[h]) return k;
                 if (k < w1) slot[h] = x;
             }
@@ -463,12 +520,13 @@ hipError_t adamw(const haste_param_t *p, int64_t n, const haste_adamw_opts_t &o,
     l.step_dev = o.step_dev;
     l.grad_scale = o.grad_scale;
     l.count = 0;
+    l.start[0] = 0;
     int64_t grid = 0;
     for (int64_t k = 0; k <= n; ++k) {
         // a run's tensors have consecutive numbers, so one of no values keeps its slot in it
         const int64_t c = k < n ? cdiv(p[k].n, kChunk) : 0;
         if (l.count > 0 && (k == n || l.count == kListMax || grid + c > kMaxGrid)) {
-            if (grid > 0) hipLaunchKernelGGL(k_adamw, dim3((unsigned)grid), dim3(kThreads), 0, s, l);
+            if (grid > 0) hipLaunchKernelGGL(k_adamw, dim3((unsigned)grid), dim3(kStepThreads), 0, s, l);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
             grid = 0;
@@ -477,20 +535,19 @@ hipError_t adamw(const haste_param_t *p, int64_t n, const haste_adamw_opts_t &o,
         if (k == n) break;
         if (l.count == 0) l.first = (uint32_t)k;
         StepTensor &t = l.t[l.count];
-        t.W = p[k].W;
-        t.W32 = p[k].W32;
-        t.grad = p[k].grad;
-        t.m = p[k].m;
-        t.v = p[k].v;
-        t.scale = p[k].scale;
-        t.n = p[k].n;
+        t.put(0, p[k].W);
+        t.put(1, p[k].W32);
+        t.put(2, p[k].grad);
+        t.put(3, p[k].m);
+        t.put(4, p[k].v);
+        t.put(5, p[k].state_bits == 8 ? p[k].scale : nullptr);
         t.lr_scale = p[k].lr_scale;
         t.weight_decay = p[k].weight_decay;
-        t.kind = (p[k].dtype == HASTE_DTYPE_BF16 ? kBf16 : 0) | (p[k].W32 ? kMaster : 0) |
-                 (p[k].grad_dtype == HASTE_DTYPE_BF16 ? kGradBf16 : 0) | (p[k].state_bits == 8 ? kBits8 : 0);
-        l.start[l.count] = (uint32_t)grid;
-        ++l.count;
+        const int kind = (p[k].dtype == HASTE_DTYPE_BF16 ? kBf16 : 0) | (p[k].W32 ? kMaster : 0) |
+                         (p[k].grad_dtype == HASTE_DTYPE_BF16 ? kGradBf16 : 0) | (p[k].state_bits == 8 ? kBits8 : 0);
+        t.last = (uint32_t)(p[k].n - (c - 1) * kChunk) | (uint32_t)kind << 16;
         grid += c;
+        l.start[++l.count] = (uint32_t)grid;
     }
     return hipSuccess;
 }
