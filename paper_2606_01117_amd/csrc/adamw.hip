@@ -172,20 +172,35 @@ constexpr int kRun = 4;
 typedef float vec4f_t __attribute__((ext_vector_type(4)));
 typedef uint32_t vec2u_t __attribute__((ext_vector_type(2)));
 
+// STREAM: past the caches, for what is not used again before the next step
+template <bool STREAM, typename V>
+__device__ __forceinline__ V load_vec(const V *p) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+template <bool STREAM, typename V>
+__device__ __forceinline__ void store_vec(V *p, V v) {
+    if constexpr (STREAM) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+template <bool STREAM = true>
 __device__ __forceinline__ void load_run(const float *p, float (&v)[kRun]) {
-    const vec4f_t a = __builtin_nontemporal_load(reinterpret_cast<const vec4f_t *>(p));
+    const vec4f_t a = load_vec<STREAM>(reinterpret_cast<const vec4f_t *>(p));
     v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
 }
+template <bool STREAM = true>
 __device__ __forceinline__ void load_run(const bf16_t *p, float (&v)[kRun]) {
-    const vec2u_t a = __builtin_nontemporal_load(reinterpret_cast<const vec2u_t *>(p));
+    const vec2u_t a = load_vec<STREAM>(reinterpret_cast<const vec2u_t *>(p));
     v[0] = __uint_as_float(a.x << 16), v[1] = __uint_as_float(a.x & 0xffff0000u);
     v[2] = __uint_as_float(a.y << 16), v[3] = __uint_as_float(a.y & 0xffff0000u);
 }
+template <bool STREAM = true>
 __device__ __forceinline__ void store_run(float *p, const float (&v)[kRun]) {
-    __builtin_nontemporal_store(vec4f_t{v[0], v[1], v[2], v[3]}, reinterpret_cast<vec4f_t *>(p));
+    store_vec<STREAM>(reinterpret_cast<vec4f_t *>(p), vec4f_t{v[0], v[1], v[2], v[3]});
 }
+template <bool STREAM = true>
 __device__ __forceinline__ void store_run(bf16_t *p, const float (&v)[kRun]) {
-    __builtin_nontemporal_store(vec2u_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}, reinterpret_cast<vec2u_t *>(p));
+    store_vec<STREAM>(reinterpret_cast<vec2u_t *>(p), vec2u_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])});
 }
 
 // ---- moments in 8 bits ------------------------------------------------------------------------------
@@ -300,7 +315,7 @@ __device__ __forceinline__ void step_values(float (&w)[N], const float (&g)[N], 
 
 // Values i0 .. i0 + n of tensor t (number k of the list), a chunk.  The tensor's whole blocks of 32 go in runs of four
 // a lane; its last, partial block one value a lane, on the workgroup's last wave.
-template <int KIND>
+template <int KIND, bool KEEP>
 __device__ __forceinline__ void step_chunk(const StepTensor &t, const StepList &l, const Scalars &c, uint32_t k, int64_t i0,
                                            uint32_t n) {
     typedef std::conditional_t<(KIND & kBf16) != 0, bf16_t, float> TW;
@@ -319,7 +334,7 @@ __device__ __forceinline__ void step_chunk(const StepTensor &t, const StepList &
         float w[kRun], g[kRun], m[kRun], v[kRun], r[kRun];
         load_run(G + i, g);
         if constexpr (MASTER) load_run(W32 + i, w);
-        else load_run(W + i, w);
+        else load_run<!KEEP>(W + i, w);
         if constexpr (B8) {
             const uint32_t sc = S[i / kBlock], qm = __builtin_nontemporal_load(QM + i / 4),
                            qv = __builtin_nontemporal_load(QV + i / 4);
@@ -335,7 +350,7 @@ __device__ __forceinline__ void step_chunk(const StepTensor &t, const StepList &
         }
         step_values(w, g, m, v, r, l, c, lr, wd);
         if constexpr (MASTER) store_run(W32 + i, w);
-        store_run(W + i, w);
+        store_run<!KEEP>(W + i, w);
         if constexpr (B8) {
             const uint32_t sm = block_scale(m), sv = block_scale(r);
             const uint64_t z = splitmix64_at(c.key, ((uint64_t)k << 40) + ((uint64_t)i0 + i) / 4);
@@ -392,6 +407,8 @@ __device__ __forceinline__ void step_chunk(const StepTensor &t, const StepList &
     }
 }
 
+// KEEP: the weights go through the caches.
+template <bool KEEP>
 __global__ __launch_bounds__(kStepThreads) void k_adamw(StepList l) {
     Scalars c = {l.lr, l.rbc1, l.rbc2, 1.0f, 0};
     if (l.grad_scale) {
@@ -412,19 +429,19 @@ __global__ __launch_bounds__(kStepThreads) void k_adamw(StepList l) {
     const int64_t i0 = (int64_t)(blockIdx.x - l.start[k]) * kChunk;
     const uint32_t no = l.first + (uint32_t)k, n = blockIdx.x + 1 < l.start[k + 1] ? (uint32_t)kChunk : t.last & 0xffffu;
     switch (t.last >> 16) {
-    case 0: step_chunk<0>(t, l, c, no, i0, n); break;
-    case kBf16: step_chunk<kBf16>(t, l, c, no, i0, n); break;
-    case kBf16 | kMaster: step_chunk<kBf16 | kMaster>(t, l, c, no, i0, n); break;
-    case kGradBf16: step_chunk<kGradBf16>(t, l, c, no, i0, n); break;
-    case kGradBf16 | kBf16: step_chunk<kGradBf16 | kBf16>(t, l, c, no, i0, n); break;
-    case kGradBf16 | kBf16 | kMaster: step_chunk<kGradBf16 | kBf16 | kMaster>(t, l, c, no, i0, n); break;
-    case kBits8: step_chunk<kBits8>(t, l, c, no, i0, n); break;
-    case kBits8 | kBf16: step_chunk<kBits8 | kBf16>(t, l, c, no, i0, n); break;
-    case kBits8 | kBf16 | kMaster: step_chunk<kBits8 | kBf16 | kMaster>(t, l, c, no, i0, n); break;
-    case kBits8 | kGradBf16: step_chunk<kBits8 | kGradBf16>(t, l, c, no, i0, n); break;
-    case kBits8 | kGradBf16 | kBf16: step_chunk<kBits8 | kGradBf16 | kBf16>(t, l, c, no, i0, n); break;
+    case 0: step_chunk<0, KEEP>(t, l, c, no, i0, n); break;
+    case kBf16: step_chunk<kBf16, KEEP>(t, l, c, no, i0, n); break;
+    case kBf16 | kMaster: step_chunk<kBf16 | kMaster, KEEP>(t, l, c, no, i0, n); break;
+    case kGradBf16: step_chunk<kGradBf16, KEEP>(t, l, c, no, i0, n); break;
+    case kGradBf16 | kBf16: step_chunk<kGradBf16 | kBf16, KEEP>(t, l, c, no, i0, n); break;
+    case kGradBf16 | kBf16 | kMaster: step_chunk<kGradBf16 | kBf16 | kMaster, KEEP>(t, l, c, no, i0, n); break;
+    case kBits8: step_chunk<kBits8, KEEP>(t, l, c, no, i0, n); break;
+    case kBits8 | kBf16: step_chunk<kBits8 | kBf16, KEEP>(t, l, c, no, i0, n); break;
+    case kBits8 | kBf16 | kMaster: step_chunk<kBits8 | kBf16 | kMaster, KEEP>(t, l, c, no, i0, n); break;
+    case kBits8 | kGradBf16: step_chunk<kBits8 | kGradBf16, KEEP>(t, l, c, no, i0, n); break;
+    case kBits8 | kGradBf16 | kBf16: step_chunk<kBits8 | kGradBf16 | kBf16, KEEP>(t, l, c, no, i0, n); break;
     case kBits8 | kGradBf16 | kBf16 | kMaster:
-        step_chunk<kBits8 | kGradBf16 | kBf16 | kMaster>(t, l, c, no, i0, n);
+        step_chunk<kBits8 | kGradBf16 | kBf16 | kMaster, KEEP>(t, l, c, no, i0, n);
         break;
     }
 }
@@ -499,8 +516,16 @@ int64_t adamw_repeated(const haste_param_t *p, int64_t n) {
     return -1;
 }
 
+// Gradients and moments are not used again before the next step and go past the caches, so do weights that the
+// memory-side cache could not hold; others stay there for the next forward pass (58M fp32 weights: 274 us past the
+// caches, 236 through them; 239M bf16 weights with 8-bit moments: 460 and 484).
+constexpr int64_t kKeepBytes = (int64_t)256 << 20;
+
 hipError_t adamw(const haste_param_t *p, int64_t n, const haste_adamw_opts_t &o, hipStream_t s) {
     StepList l;
+    int64_t bytes = 0;
+    for (int64_t k = 0; k < n; ++k) bytes += p[k].n * (p[k].dtype == HASTE_DTYPE_BF16 ? 2 : 4);
+    const auto kernel = bytes <= kKeepBytes ? k_adamw<true> : k_adamw<false>;
     l.b1 = (float)o.beta1;
     l.c1 = (float)(1.0 - o.beta1);
     l.b2 = (float)o.beta2;
@@ -526,7 +551,7 @@ hipError_t adamw(const haste_param_t *p, int64_t n, const haste_adamw_opts_t &o,
         // a run's tensors have consecutive numbers, so one of no values keeps its slot in it
         const int64_t c = k < n ? cdiv(p[k].n, kChunk) : 0;
         if (l.count > 0 && (k == n || l.count == kListMax || grid + c > kMaxGrid)) {
-            if (grid > 0) hipLaunchKernelGGL(k_adamw, dim3((unsigned)grid), dim3(kStepThreads), 0, s, l);
+            if (grid > 0) hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(kStepThreads), 0, s, l);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
             grid = 0;

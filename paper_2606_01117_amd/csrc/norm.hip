@@ -1,8 +1,13 @@
 // Layer norm of rows, forward and backward, with the reduction of the gradients of weight and bias.
 //
-// A row belongs to a team of 16, 64, 256 or 1024 threads, which hold it in registers: every value is read once
-// and every sum is taken from the registers, the squares around the row's mean.  A thread holds NC runs of
-// four consecutive values, TEAM runs apart.  Rows wider than kWideF go through a loop that reads them again.
+// A row belongs to a team of 16, 64, 256, 512 or 1024 threads, which hold it in registers: every value is read
+// once and every sum is taken from the registers, the squares around the row's mean.  A thread holds NC runs of
+// four consecutive values, TEAM runs apart.  Rows wider than kWideF, or of fewer than four values, go through a
+// loop that reads them again.
+//
+// No load hangs on a branch (a load behind one is waited for at its end, and so one after the other): a run that
+// would reach past its row starts at the row's last four values instead, and what the run before it holds too is
+// masked in the sums and not stored; a row past the last is read as the last one.
 #include "common.hpp"
 
 namespace {
@@ -18,30 +23,21 @@ typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef u32x4_t u32x4_el_t __attribute__((aligned(4)));
 typedef u32x2_t u32x2_el_t __attribute__((aligned(2)));
 
-// n values of the four are there; the others read as zero
-__device__ __forceinline__ Raw4<float> load4(const float *p, int64_t n) {
-    Raw4<float> r = {};
-    if (n >= 4) {
-        const u32x4_t v = *reinterpret_cast<const u32x4_el_t *>(p);
-        r.w[0] = v.x, r.w[1] = v.y, r.w[2] = v.z, r.w[3] = v.w;
-    } else {
-#pragma unroll
-        for (int j = 0; j < 3; ++j)
-            if (j < n) r.w[j] = __float_as_uint(p[j]);
-    }
-    return r;
+// STREAM: past the caches, not read again
+template <bool STREAM, typename V>
+__device__ __forceinline__ V load_vec(const V *p) {
+    if constexpr (STREAM) return __builtin_nontemporal_load(p);
+    else return *p;
 }
-__device__ __forceinline__ Raw4<bf16_t> load4(const bf16_t *p, int64_t n) {
-    Raw4<bf16_t> r = {};
-    if (n >= 4) {
-        const u32x2_t v = *reinterpret_cast<const u32x2_el_t *>(p);
-        r.w[0] = v.x, r.w[1] = v.y;
-    } else {
-        if (n > 0) r.w[0] = p[0];
-        if (n > 1) r.w[0] |= (uint32_t)p[1] << 16;
-        if (n > 2) r.w[1] = p[2];
-    }
-    return r;
+template <bool STREAM = false>
+__device__ __forceinline__ Raw4<float> load4(const float *p) {
+    const u32x4_t v = load_vec<STREAM>(reinterpret_cast<const u32x4_el_t *>(p));
+    return {{v.x, v.y, v.z, v.w}};
+}
+template <bool STREAM = false>
+__device__ __forceinline__ Raw4<bf16_t> load4(const bf16_t *p) {
+    const u32x2_t v = load_vec<STREAM>(reinterpret_cast<const u32x2_el_t *>(p));
+    return {{v.x, v.y}};
 }
 __device__ __forceinline__ void unpack4(const Raw4<float> &r, float (&v)[4]) {
 #pragma unroll
@@ -51,25 +47,29 @@ __device__ __forceinline__ void unpack4(const Raw4<bf16_t> &r, float (&v)[4]) {
     v[0] = __uint_as_float(r.w[0] << 16), v[1] = __uint_as_float(r.w[0] & 0xffff0000u);
     v[2] = __uint_as_float(r.w[1] << 16), v[3] = __uint_as_float(r.w[1] & 0xffff0000u);
 }
-__device__ __forceinline__ void store4(float *p, const float (&v)[4], int64_t n) {
-    if (n >= 4) {
-        const u32x4_t w = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-        *reinterpret_cast<u32x4_el_t *>(p) = w;
-    } else {
-#pragma unroll
-        for (int j = 0; j < 3; ++j)
-            if (j < n) p[j] = v[j];
-    }
+__device__ __forceinline__ void store4(float *p, const float (&v)[4]) {
+    const u32x4_t w = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    *reinterpret_cast<u32x4_el_t *>(p) = w;
 }
-__device__ __forceinline__ void store4(bf16_t *p, const float (&v)[4], int64_t n) {
-    if (n >= 4) {
-        const u32x2_t w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-        *reinterpret_cast<u32x2_el_t *>(p) = w;
-    } else {
-#pragma unroll
-        for (int j = 0; j < 3; ++j)
-            if (j < n) p[j] = f32_to_bf16(v[j]);
+__device__ __forceinline__ void store4(bf16_t *p, const float (&v)[4]) {
+    const u32x2_t w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    *reinterpret_cast<u32x2_el_t *>(p) = w;
+}
+
+// A run of a row of F values: it starts at the value `at`, and its own values are those from `skip` on.
+struct Run {
+    int at, skip;
+    __device__ __forceinline__ Run(int run, int F) {
+        const int f = 4 * run;
+        at = f < F - 4 ? f : F - 4;
+        skip = f - at;                          // 0, of a last one 1 .. 3, of one past the row 4 or more
     }
+    __device__ __forceinline__ bool any() const { return skip < 4; }
+};
+// stores the run; its neighbour's values, which it holds too, are the same
+template <typename T>
+__device__ __forceinline__ void store4(T *row, const Run &r, const float (&v)[4]) {
+    if (r.any()) store4(row + r.at, v);
 }
 
 // ---- sums over a team -------------------------------------------------------------------------------
@@ -120,6 +120,8 @@ __device__ __forceinline__ void team_sum(float (&v)[N], float *red, int &turn) {
 }
 
 // ---- forward ----------------------------------------------------------------------------------------
+// X is stored through the caches: whoever reads it next finds it there (65536 x 768 bf16: 35 us past them instead
+// of 43, but with the product X W of 768 columns behind it 124 us instead of 121).
 template <typename TH, typename TX, int TEAM, int NC>
 __global__ __launch_bounds__(TEAM > 256 ? TEAM : 256) void k_ln_fwd(int64_t B, int F, const TH *H, int64_t ldh,
                                                                     const float *__restrict__ weight,
@@ -129,51 +131,59 @@ __global__ __launch_bounds__(TEAM > 256 ? TEAM : 256) void k_ln_fwd(int64_t B, i
     __shared__ float red[2 * 16];
     int turn = 0;
     const int t = threadIdx.x % TEAM;
-    const int64_t teams = blockDim.x / TEAM;
+    const int64_t teams = blockDim.x / TEAM, next = gridDim.x * teams;
+    Raw4<TH> raw[NC];
+    auto ask = [&](int64_t b) {
+        const TH *h = H + (b < B ? b : B - 1) * ldh;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) raw[i] = load4(h + Run(i * TEAM + t, F).at);
+    };
+    ask(blockIdx.x * teams + threadIdx.x / TEAM);
     float w[NC][4], c[NC][4];
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-        const int f = 4 * (i * TEAM + t);
-        unpack4(load4(weight + f, weight ? F - f : 0), w[i]);
-        unpack4(load4(bias + f, bias ? F - f : 0), c[i]);
-        if (!weight)
-            for (int j = 0; j < 4; ++j) w[i][j] = 1.0f;
+        const Run r(i * TEAM + t, F);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[i][j] = 1.0f, c[i][j] = 0.0f;
+        if (weight) unpack4(load4(weight + r.at), w[i]);
+        if (bias) unpack4(load4(bias + r.at), c[i]);
     }
-    // every team of a workgroup goes round as often as the first one, for the barriers
-    for (int64_t b0 = blockIdx.x * teams; b0 < B; b0 += gridDim.x * teams) {
+    // every team of a workgroup goes round as often as the first one, for the barriers; a row's values are asked
+    // for before the row before it is summed
+    for (int64_t b0 = blockIdx.x * teams; b0 < B; b0 += next) {
         const int64_t b = b0 + threadIdx.x / TEAM;
-        const bool in = b < B;
-        const TH *h = H + (in ? b : b0) * ldh;
         float v[NC][4], s[1] = {0.0f};
 #pragma unroll
-        for (int i = 0; i < NC; ++i) {
-            const int f = 4 * (i * TEAM + t);
-            unpack4(load4(h + f, F - f), v[i]);
-        }
+        for (int i = 0; i < NC; ++i) unpack4(raw[i], v[i]);
+        ask(b + next);
 #pragma unroll
-        for (int i = 0; i < NC; ++i) s[0] += (v[i][0] + v[i][1]) + (v[i][2] + v[i][3]);
+        for (int i = 0; i < NC; ++i) {
+            const int skip = i == NC - 1 ? Run(i * TEAM + t, F).skip : 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[0] += j < skip ? 0.0f : v[i][j];
+        }
         team_sum<TEAM>(s, red, turn);
         const float mu = s[0] / (float)F;
         s[0] = 0.0f;
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-            const int f = 4 * (i * TEAM + t);
+            const int skip = i == NC - 1 ? Run(i * TEAM + t, F).skip : 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                v[i][j] = f + j < F ? v[i][j] - mu : 0.0f;
-                s[0] = __fmaf_rn(v[i][j], v[i][j], s[0]);
+                v[i][j] -= mu;
+                const float d = j < skip ? 0.0f : v[i][j];
+                s[0] = __fmaf_rn(d, d, s[0]);
             }
         }
         team_sum<TEAM>(s, red, turn);
         const float rs = 1.0f / sqrtf(s[0] / (float)F + eps);
-        if (in) {
+        if (b < B) {
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
-                const int f = 4 * (i * TEAM + t);
                 float o[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) o[j] = __fmaf_rn(v[i][j] * rs, w[i][j], c[i][j]);
-                store4(X + b * ldx + f, o, F - f);
+                store4(X + b * ldx, Run(i * TEAM + t, F), o);
             }
             if (mean && t == 0) {
                 mean[b] = mu;
@@ -184,102 +194,193 @@ __global__ __launch_bounds__(TEAM > 256 ? TEAM : 256) void k_ln_fwd(int64_t B, i
 }
 
 // ---- backward ---------------------------------------------------------------------------------------
-// Both sums of a row and its gradient from one read of H and dX; where the gradients of weight and bias are
-// asked for (WG), every thread adds its values' terms over the team's rows in registers, the teams of a
-// workgroup are added in LDS, and part[workgroup][0][f] and part[workgroup][1][f] are its sums.
-template <typename TH, typename TD, int TEAM, int NC, bool WG>
-__global__ __launch_bounds__(1024) void k_ln_bwd(int64_t B, int F, const TH *__restrict__ H, int64_t ldh,
-                                                 const float *__restrict__ weight, const float *__restrict__ mean,
-                                                 const float *__restrict__ rstd, const TD *dX, int64_t lddx, TH *dH,
-                                                 int64_t lddh, float *__restrict__ part) {
+// The arrays of a backward call.
+template <typename TH, typename TD>
+struct Bwd {
+    int64_t B;
+    int F;
+    const TH *H;
+    int64_t ldh;
+    const float *weight, *mean, *rstd;
+    const TD *dX;
+    int64_t lddx;
+    TH *dH;
+    int64_t lddh;
+};
+
+// Rows first, first + next, ... of a team: both sums of a row and its gradient from one read of H and dX; where
+// WG, every thread adds its values' terms of dweight and dbias over the rows in aw and ab.  H and dX are read for
+// the last time here, so rows of whole 16-byte accesses go past the caches (STREAM: 65536 x 768 bf16 55 us, 63
+// through them); others share their accesses' lines with their neighbours and stay (4099 x 1003 fp32: 21.3 us
+// past them, 20.3).
+template <typename TH, typename TD, int TEAM, int NC, bool WG, bool STREAM>
+__device__ __forceinline__ void bwd_rows(const Bwd<TH, TD> &a, int64_t b0, int64_t next, float (&aw)[NC][4],
+                                         float (&ab)[NC][4]) {
     __shared__ float red[2 * 16 * 2];
-    extern __shared__ float4 lds[];             // [teams][F] floats, rows of whole float4
     int turn = 0;
-    const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM, teams = blockDim.x / TEAM;
-    float w[NC][4], aw[NC][4], ab[NC][4];
+    const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM, F = a.F;
+    Raw4<TH> rh[NC];
+    Raw4<TD> rd[NC];
+    float mu_next, rs_next;
+    auto ask = [&](int64_t b) {
+        const int64_t k = b < a.B ? b : a.B - 1;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const Run r(i * TEAM + t, F);
+            rh[i] = load4<STREAM>(a.H + k * a.ldh + r.at);
+            rd[i] = load4<STREAM>(a.dX + k * a.lddx + r.at);
+        }
+        mu_next = a.mean[k];
+        rs_next = a.rstd[k];
+    };
+    // a row's values are asked for before the row before it is summed, where 128 registers a thread hold both
+    constexpr bool EARLY = !WG || NC < 4;
+    if (EARLY) ask(b0 + team);
+    float w[NC][4];
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-        const int f = 4 * (i * TEAM + t);
-        unpack4(load4(weight + f, weight ? F - f : 0), w[i]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if (!weight) w[i][j] = 1.0f;
+            w[i][j] = 1.0f;
             aw[i][j] = ab[i][j] = 0.0f;
         }
+        if (a.weight) unpack4(load4(a.weight + Run(i * TEAM + t, F).at), w[i]);
     }
-    for (int64_t b0 = (int64_t)blockIdx.x * teams; b0 < B; b0 += (int64_t)gridDim.x * teams) {
-        const bool in = b0 + team < B;
-        const int64_t b = in ? b0 + team : b0;
-        const TH *h = H + b * ldh;
-        const TD *d = dX + b * lddx;
+    for (; b0 < a.B; b0 += next) {
+        const int64_t b = b0 + team;
+        const bool in = b < a.B;
+        if (!EARLY) ask(b);
         float x[NC][4], g[NC][4];
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-            const int f = 4 * (i * TEAM + t);
-            unpack4(load4(h + f, F - f), x[i]);
-            unpack4(load4(d + f, in ? F - f : 0), g[i]);      // a row that is not there adds zeros
+            unpack4(rh[i], x[i]);
+            unpack4(rd[i], g[i]);
         }
-        const float mu = mean[b], rs = rstd[b];
-        float s[2] = {0.0f, 0.0f};
+        const float mu = mu_next, rs = rs_next;
+        if (EARLY) ask(b + next);
 #pragma unroll
         for (int i = 0; i < NC; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x[i][j] = (x[i][j] - mu) * rs;
-                if constexpr (WG) {
-                    aw[i][j] = in ? __fmaf_rn(g[i][j], x[i][j], aw[i][j]) : aw[i][j];
+            for (int j = 0; j < 4; ++j) x[i][j] = (x[i][j] - mu) * rs;
+        if (WG && in) {
+#pragma unroll
+            for (int i = 0; i < NC; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    aw[i][j] = __fmaf_rn(g[i][j], x[i][j], aw[i][j]);
                     ab[i][j] += g[i][j];
                 }
+        }
+        if (!a.dH) continue;
+        float s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int skip = i == NC - 1 ? Run(i * TEAM + t, F).skip : 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
                 g[i][j] *= w[i][j];
-                s[0] += g[i][j];
-                s[1] = 4 * (i * TEAM + t) + j < F ? __fmaf_rn(g[i][j], x[i][j], s[1]) : s[1];
+                const float q = j < skip ? 0.0f : g[i][j], p = j < skip ? 0.0f : x[i][j];
+                s[0] += q;
+                s[1] = __fmaf_rn(q, p, s[1]);
             }
-        if (!dH) continue;
+        }
         team_sum<TEAM>(s, red, turn);
         const float m0 = s[0] / (float)F, m1 = s[1] / (float)F;
         if (in) {
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
-                const int f = 4 * (i * TEAM + t);
                 float o[4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) o[j] = (g[i][j] - m0 - x[i][j] * m1) * rs;
-                store4(dH + b * lddh + f, o, F - f);
+                store4(a.dH + b * a.lddh, Run(i * TEAM + t, F), o);
             }
         }
     }
-    if constexpr (WG) {
-        const int F4 = (F + 3) / 4;
+}
+
+// stores a run's own values alone
+__device__ __forceinline__ void store_own(float *out, const Run &r, const float (&v)[4]) {
+    if (r.skip == 0) {
+        store4(out + r.at, v);
+        return;
+    }
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            float *out = part + (2 * (int64_t)blockIdx.x + k) * F;
-            if (teams == 1) {
+    for (int j = 1; j < 4; ++j)
+        if (j >= r.skip) out[r.at + j] = v[j];
+}
+
+// Rows, and (part not NULL) part[workgroup][0][f] and part[workgroup][1][f], the workgroup's sums for dweight and
+// dbias: its teams' terms, added in LDS run by run.
+template <typename TH, typename TD, int TEAM, int NC, bool STREAM>
+__global__ __launch_bounds__(1024) void k_ln_bwd(Bwd<TH, TD> a, float *__restrict__ part) {
+    extern __shared__ float4 lds[];             // [teams][runs]
+    const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM, teams = blockDim.x / TEAM, F = a.F;
+    float aw[NC][4], ab[NC][4];
+    bwd_rows<TH, TD, TEAM, NC, true, STREAM>(a, (int64_t)blockIdx.x * teams, (int64_t)gridDim.x * teams, aw, ab);
+    if (!part) return;
+    const int runs = (F + 3) / 4;
 #pragma unroll
-                for (int i = 0; i < NC; ++i) {
-                    const int f = 4 * (i * TEAM + t);
-                    store4(out + f, k ? ab[i] : aw[i], F - f);
-                }
-                continue;
-            }
-            if (k) __syncthreads();
+    for (int k = 0; k < 2; ++k) {
+        float *out = part + (2 * (int64_t)blockIdx.x + k) * F;
+        if (teams == 1) {
 #pragma unroll
-            for (int i = 0; i < NC; ++i) {
-                const int q = i * TEAM + t;
-                const float *v = k ? ab[i] : aw[i];
-                if (q < F4) lds[team * F4 + q] = make_float4(v[0], v[1], v[2], v[3]);
+            for (int i = 0; i < NC; ++i) store_own(out, Run(i * TEAM + t, F), k ? ab[i] : aw[i]);
+            continue;
+        }
+        if (k) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int q = i * TEAM + t;
+            const float *v = k ? ab[i] : aw[i];
+            if (q < runs) lds[team * runs + q] = make_float4(v[0], v[1], v[2], v[3]);
+        }
+        __syncthreads();
+        for (int q = threadIdx.x; q < runs; q += blockDim.x) {
+            float4 s = lds[q];
+            for (int r = 1; r < teams; ++r) {
+                const float4 v = lds[r * runs + q];
+                s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
             }
-            __syncthreads();
-            for (int q = threadIdx.x; q < F4; q += blockDim.x) {
-                float4 a = lds[q];
-                for (int r = 1; r < teams; ++r) {
-                    const float4 v = lds[r * F4 + q];
-                    a.x += v.x, a.y += v.y, a.z += v.z, a.w += v.w;
-                }
-                const float v[4] = {a.x, a.y, a.z, a.w};
-                store4(out + 4 * q, v, F - 4 * q);
-            }
+            const float v[4] = {s.x, s.y, s.z, s.w};
+            store_own(out, Run(q, F), v);
         }
     }
+}
+
+// Few rows, dH not in dX's place: one launch.  The workgroups from row_blocks on take eight columns each, straight
+// to dweight and dbias, every thread of a column blockDim / 8 rows apart.
+template <typename TH, typename TD, int TEAM, int NC>
+__global__ __launch_bounds__(1024) void k_ln_bwd_few(Bwd<TH, TD> a, unsigned row_blocks, float *__restrict__ dweight,
+                                                     float *__restrict__ dbias, int beta) {
+    __shared__ float sw[1024], sb[1024];
+    if (blockIdx.x < row_blocks) {
+        const int teams = blockDim.x / TEAM;
+        float aw[NC][4], ab[NC][4];
+        bwd_rows<TH, TD, TEAM, NC, false, false>(a, (int64_t)blockIdx.x * teams, (int64_t)row_blocks * teams, aw, ab);
+        return;
+    }
+    const int64_t f = (int64_t)(blockIdx.x - row_blocks) * 8 + (threadIdx.x & 7);
+    float w = 0.0f, c = 0.0f;
+    if (f < a.F) {
+#pragma unroll 8
+        for (int64_t b = threadIdx.x >> 3; b < a.B; b += blockDim.x >> 3) {
+            const float d = load_f32(a.dX + b * a.lddx, f);
+            w = __fmaf_rn(d, (load_f32(a.H + b * a.ldh, f) - a.mean[b]) * a.rstd[b], w);
+            c += d;
+        }
+    }
+    sw[threadIdx.x] = w;
+    sb[threadIdx.x] = c;
+    for (unsigned n = blockDim.x / 2; n >= 8; n /= 2) {
+        __syncthreads();
+        if (threadIdx.x < n) {
+            sw[threadIdx.x] = w += sw[threadIdx.x + n];
+            sb[threadIdx.x] = c += sb[threadIdx.x + n];
+        }
+    }
+    if (threadIdx.x >= 8 || f >= a.F) return;
+    if (dweight) dweight[f] = beta ? dweight[f] + w : w;
+    if (dbias) dbias[f] = beta ? dbias[f] + c : c;
 }
 
 // dweight, dbias (either may be NULL) from the workgroups' sums: 64 columns a workgroup, its sixteen waves a
@@ -406,44 +507,59 @@ __global__ __launch_bounds__(kThreads) void k_ln_wgrad_wide(int64_t B, int64_t F
 
 // ---- which team takes a row ---------------------------------------------------------------------------
 constexpr int64_t kWideF = 8192;       // rows beyond it are not held in registers
+bool held(int64_t F) { return F >= 4 && F <= kWideF; }
 constexpr int kMaxRowBlocks = 65536;   // workgroups of the kernels for them; more rows go round
 
-int team_of(int64_t F) { return F <= 256 ? 16 : F <= 1024 ? 64 : F <= 2048 ? 256 : 1024; }
+constexpr int fwd_team(int64_t F) { return F <= 256 ? 16 : F <= 1024 ? 64 : F <= 4096 ? 256 : 1024; }
+constexpr int bwd_team(int64_t F) { return F <= 256 ? 16 : F <= 1024 ? 64 : F <= 2048 ? 256 : F <= 4096 ? 512 : 1024; }
 
-// f(team, runs of four values a thread) for rows of F <= kWideF values
-template <typename F>
+// f(team, runs of four values a thread), the team one of the constants that team_of gives up to kWideF
+template <int LEAST, int MOST, typename F>
+void with_runs(int64_t n, F &&f) {
+    if constexpr (LEAST < MOST)
+        if (n > LEAST) return with_runs<LEAST + 1, MOST>(n, f);
+    f(std::integral_constant<int, LEAST>{});
+}
+template <int TEAM, int MOST, typename F>
 void with_team(int64_t width, F &&f) {
-    auto go = [&](auto team, auto most) {
-        const int64_t n = haste::cdiv(width, 4 * team);
-        if (n <= 1) f(team, std::integral_constant<int, 1>{});
-        else if (n == 2) f(team, std::integral_constant<int, 2>{});
-        if constexpr (most > 2) {
-            if (n == 3) f(team, std::integral_constant<int, 3>{});
-            else if (n == 4) f(team, std::integral_constant<int, 4>{});
-        }
-    };
-    typedef std::integral_constant<int, 2> two;
-    typedef std::integral_constant<int, 4> four;
-    switch (team_of(width)) {
-    case 16: go(std::integral_constant<int, 16>{}, four{}); break;
-    case 64: go(std::integral_constant<int, 64>{}, four{}); break;
-    case 256: go(std::integral_constant<int, 256>{}, two{}); break;
-    default: go(std::integral_constant<int, 1024>{}, two{});
+    with_runs<1, MOST>(haste::cdiv(width, 4 * TEAM), [&](auto nc) { f(std::integral_constant<int, TEAM>{}, nc); });
+}
+template <typename F>
+void with_fwd_team(int64_t width, F &&f) {
+    switch (fwd_team(width)) {
+    case 16: return with_team<16, 4>(width, f);
+    case 64: return with_team<64, 4>(width, f);
+    case 256: return with_team<256, 4>(width, f);
+    default: return with_team<1024, 2>(width, f);
+    }
+}
+template <typename F>
+void with_bwd_team(int64_t width, F &&f) {
+    switch (bwd_team(width)) {
+    case 16: return with_team<16, 4>(width, f);
+    case 64: return with_team<64, 4>(width, f);
+    case 256: return with_team<256, 2>(width, f);
+    case 512: return with_team<512, 2>(width, f);
+    default: return with_team<1024, 2>(width, f);
     }
 }
 
-// The backward kernel's workgroups.  Each leaves one row of sums, so many rows take 1024 threads a workgroup and
-// no more workgroups than CUs; few rows take 256 threads, to spread over the CUs.
+// The backward kernel's workgroups.  Each leaves one row of sums, so there are no more than CUs, and a CU's rows
+// share its workgroup's teams, up to 1024 threads, about two rows a team at least (4099 x 1003 fp32 in up to 1024
+// workgroups of 256 threads, a row a team: 20.3 us, so 16.9).
 struct BwdShape {
     int threads;
     int64_t blocks;
 };
 BwdShape bwd_shape(int64_t B, int64_t F) {
-    const int team = team_of(F);
-    const int threads = team > 256 || B * team >= (int64_t)2 * 256 * 1024 ? 1024 : 256;
-    const int64_t want = haste::cdiv(B, threads / team), most = 256 * (1024 / threads);
-    return {threads, want < most ? want : most};
+    const int team = bwd_team(F);
+    int threads = team > 256 ? team : 256;
+    while (threads < 1024 && B > (int64_t)256 * 2 * (threads / team)) threads *= 2;
+    const int64_t want = haste::cdiv(B, threads / team);
+    return {threads, want < 256 ? want : 256};
 }
+// Rows whose column sums a second pass over them, from the caches, forms as fast as partial sums would be added.
+constexpr int64_t kFewRows = 512;
 
 int64_t wide_parts(int64_t B) {
     const int64_t n = haste::cdiv(B, 64);
@@ -468,12 +584,12 @@ hipError_t ln_fwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t 
         with_type(dtype_x, [&](auto tx) {
             typedef decltype(th) TH;
             typedef decltype(tx) TX;
-            if (F > kWideF) {
+            if (!held(F)) {
                 hipLaunchKernelGGL((k_ln_fwd_wide<TH, TX>), dim3((unsigned)(B < kMaxRowBlocks ? B : kMaxRowBlocks)),
                                    dim3(kThreads), 0, s, B, F, (const TH *)H, ldh, weight, bias, eps, (TX *)X, ldx, mean, rstd);
                 return;
             }
-            with_team(F, [&](auto team, auto nc) {
+            with_fwd_team(F, [&](auto team, auto nc) {
                 const int threads = team > 256 ? (int)team : 256;
                 const int64_t want = cdiv(B, threads / team), most = 256 * (2048 / threads);
                 hipLaunchKernelGGL((k_ln_fwd<TH, TX, team, nc>), dim3((unsigned)(want < most ? want : most)), dim3(threads), 0,
@@ -485,7 +601,7 @@ hipError_t ln_fwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t 
 }
 
 size_t ln_bwd_ws(int64_t B, int64_t F) {
-    return (size_t)((F > kWideF ? wide_parts(B) : bwd_shape(B, F).blocks) * 2 * F * 4);
+    return (size_t)((!held(F) ? wide_parts(B) : bwd_shape(B, F).blocks) * 2 * F * 4);
 }
 
 hipError_t ln_bwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t ldh, const float *weight,
@@ -494,12 +610,13 @@ hipError_t ln_bwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t 
     float *part = (float *)ws;
     const bool wg = dweight || dbias;
     const BwdShape n = bwd_shape(B, F);
-    const int64_t parts = F > kWideF ? wide_parts(B) : n.blocks;
+    const int64_t parts = !held(F) ? wide_parts(B) : n.blocks;
+    const bool few = wg && B <= kFewRows && held(F) && dH != dX;
     with_type(dtype_h, [&](auto th) {
         with_type(dtype_dx, [&](auto td) {
             typedef decltype(th) TH;
             typedef decltype(td) TD;
-            if (F > kWideF) {
+            if (!held(F)) {
                 // the sums over rows first: dH may take dX's place
                 if (wg)
                     hipLaunchKernelGGL((k_ln_wgrad_wide<TH, TD>), dim3((unsigned)cdiv(F, kWave), (unsigned)parts),
@@ -511,19 +628,29 @@ hipError_t ln_bwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t 
                                        lddx, (TH *)dH, lddh);
                 return;
             }
-            with_team(F, [&](auto team, auto nc) {
+            const auto whole = [](const void *p, int64_t ld, int64_t size) {
+                return (reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * size)) % 16 == 0;
+            };
+            const bool stream = whole(H, ldh, sizeof(TH)) && whole(dX, lddx, sizeof(TD));
+            const Bwd<TH, TD> a = {B, (int)F, (const TH *)H, ldh, weight, mean, rstd, (const TD *)dX, lddx, (TH *)dH, lddh};
+            with_bwd_team(F, [&](auto team, auto nc) {
                 const int teams = n.threads / team;
                 const size_t lds = wg && teams > 1 ? (size_t)teams * cdiv(F, 4) * 16 : 0;
-                if (wg)
-                    hipLaunchKernelGGL((k_ln_bwd<TH, TD, team, nc, true>), dim3((unsigned)n.blocks), dim3(n.threads), lds, s, B,
-                                       (int)F, (const TH *)H, ldh, weight, mean, rstd, (const TD *)dX, lddx, (TH *)dH, lddh, part);
-                else
-                    hipLaunchKernelGGL((k_ln_bwd<TH, TD, team, nc, false>), dim3((unsigned)n.blocks), dim3(n.threads), lds, s, B,
-                                       (int)F, (const TH *)H, ldh, weight, mean, rstd, (const TD *)dX, lddx, (TH *)dH, lddh, part);
+                if (few) {
+                    const unsigned rows = dH ? (unsigned)n.blocks : 0;
+                    hipLaunchKernelGGL((k_ln_bwd_few<TH, TD, team, nc>), dim3(rows + (unsigned)cdiv(F, 8)), dim3(n.threads), 0, s,
+                                       a, rows, dweight, dbias, beta);
+                } else if (stream) {
+                    hipLaunchKernelGGL((k_ln_bwd<TH, TD, team, nc, true>), dim3((unsigned)n.blocks), dim3(n.threads), lds, s, a,
+                                       wg ? part : nullptr);
+                } else {
+                    hipLaunchKernelGGL((k_ln_bwd<TH, TD, team, nc, false>), dim3((unsigned)n.blocks), dim3(n.threads), lds, s, a,
+                                       wg ? part : nullptr);
+                }
             });
         });
     });
-    if (wg)
+    if (wg && !few)
         hipLaunchKernelGGL(k_ln_wsum, dim3((unsigned)cdiv(2 * F, kWave)), dim3(1024), 0, s, part, parts, F, dweight, dbias, beta);
     return hipGetLastError();
 }
