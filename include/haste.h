@@ -392,7 +392,8 @@ int haste_head_bwd(int64_t B, int64_t F_s, int64_t H, int32_t dtype, const void 
  * elements only.  weight[F], bias[F] fp32 or NULL (ones, zeros).  mean[B], rstd[B] fp32, both or neither
  * (NULL): what haste_layer_norm_bwd takes.  X may be H where type and stride are the same.
  * Arithmetic: fp32, the squares around the row's mean; a bf16 X is rounded once.  An infinity or a NaN
- * makes its own row NaN.  eps >= 0; at 0 a row of equal values is NaN.  F >= 1; B == 0 launches nothing.
+ * makes its own row NaN.  eps >= 0; at 0 a row of equal values is NaN.  1 <= F <= 2^24; B < 2^31,
+ * B == 0 launches nothing.
  */
 int haste_layer_norm_fwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t ldh,
                          const float *weight, const float *bias, float eps, int32_t dtype_x, void *X,

@@ -388,10 +388,10 @@ def haste_layer_norm_bwd(B, F, dtype_h, H, weight, mean, rstd, dtype_dx, dX, dH=
 
 
 def _dtype_of(t, name) -> int:
-    import torch
-    if t.dtype == torch.float32:
+    torch = _torch()
+    if t.dtype is torch.float32:
         return HASTE_DTYPE_F32
-    if t.dtype == torch.bfloat16:
+    if t.dtype is torch.bfloat16:
         return HASTE_DTYPE_BF16
     raise ValueError(f"{name} must be torch.float32 or torch.bfloat16, got {t.dtype}")
 
@@ -400,49 +400,61 @@ def param(W=None, grad=None, m=None, v=None, scale=None, W32=None, lr_scale=1.0,
     """One tensor of a list for haste_grad_norm (which needs grad alone) and haste_adamw.
 
     W (fp32 or bf16), grad (fp32 or bf16), and the moments m and v: fp32, or of one byte a value (uint8, or
-    float8_e4m3fn) with scale, uint8 [ceil(n / 32), 2].  All contiguous, of n values each.  The entry keeps the
-    tensors alive."""
-    n = (grad if grad is not None else W).numel()
-    p = haste_param_t(n=n, lr_scale=lr_scale, weight_decay=weight_decay, state_bits=32)
-    p.keep = (W, grad, m, v, scale, W32)
-    for t, name in ((W, "W"), (grad, "grad"), (m, "m"), (v, "v"), (W32, "W32")):
+    float8_e4m3fn) with scale, uint8 [ceil(n / 32), 2].  All contiguous, of n values each, on the current GPU.  The
+    entry keeps the tensors alive."""
+    first = grad if grad is not None else W
+    n, device = first.numel(), _here(first, "grad" if grad is not None else "W")
+
+    def at(t, name, count):
         if t is None:
-            continue
-        if t.numel() != n:
-            raise ValueError(f"{name} has {t.numel()} values, not {n}")
-        _here(t, name)
-        setattr(p, name, _ptr(t))
-    if W is not None:
-        p.dtype = _dtype_of(W, "W")
-    if grad is not None:
-        p.grad_dtype = _dtype_of(grad, "grad")
-    if W32 is not None and _dtype_of(W32, "W32") != HASTE_DTYPE_F32:
-        raise ValueError("W32 must be torch.float32")
+            return None
+        if t.numel() != count or not t.is_contiguous():
+            raise ValueError(f"{name} must be {count} contiguous values, got {tuple(t.shape)}")
+        if t.get_device() != device:
+            _elsewhere(t, name)
+        return t.data_ptr()
+
+    bits = 32
     if m is not None and v is not None:
         if m.element_size() == 1 and v.element_size() == 1:
-            p.state_bits = 8
-            if scale is None or scale.element_size() != 1 or scale.numel() != 2 * ((n + 31) // 32):
+            bits = 8
+            if scale is None or scale.element_size() != 1:
                 raise ValueError(f"8-bit moments of {n} values need scale, uint8 [{(n + 31) // 32}, 2]")
-            _here(scale, "scale")
-            p.scale = _ptr(scale)
         elif _dtype_of(m, "m") != HASTE_DTYPE_F32 or _dtype_of(v, "v") != HASTE_DTYPE_F32:
             raise ValueError("m and v must both be torch.float32, or both of one byte a value")
+    if W32 is not None and _dtype_of(W32, "W32") != HASTE_DTYPE_F32:
+        raise ValueError("W32 must be torch.float32")
+    p = haste_param_t(at(W, "W", n), at(W32, "W32", n), at(grad, "grad", n), at(m, "m", n), at(v, "v", n),
+                      at(scale, "scale", 2 * ((n + 31) // 32)), n, lr_scale, weight_decay,
+                      0 if W is None else _dtype_of(W, "W"), 0 if grad is None else _dtype_of(grad, "grad"), bits, 0)
+    p.keep, p.device = (W, grad, m, v, scale, W32), device
     return p
 
 
 def param_list(params):
     """The array of entries that haste_grad_norm and haste_adamw take; made once, it serves every step."""
     params = list(params)
+    devices = {getattr(p, "device", None) for p in params} - {None}
+    if len(devices) > 1:
+        raise ValueError(f"the tensors of a list must be on one GPU, not on {sorted(devices)}")
     array = (haste_param_t * len(params))(*params)
     array.keep = [getattr(p, "keep", None) for p in params]
+    array.device = devices.pop() if devices else None
     return array
+
+
+def _list_here(params):
+    device = getattr(params, "device", None)
+    if device is not None and device != _torch().cuda.current_device():
+        raise ValueError(f"the list's tensors are on cuda:{device}, not on the current device "
+                         f"cuda:{_torch().cuda.current_device()}")
 
 
 def adamw_opts(lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, seed=0, lr_dev=None, step_dev=None,
                grad_scale=None) -> haste_adamw_opts_t:
     """Options of haste_adamw; the caller sets .step (and .lr) before each call.  lr_dev (fp32), step_dev (int64)
     and grad_scale (fp32, haste_grad_norm's out[1:]) are GPU tensors of one value, or None."""
-    import torch
+    torch = _torch()
     o = haste_adamw_opts_t(lr=lr, beta1=beta1, beta2=beta2, eps=eps, step=step, seed=seed & ((1 << 64) - 1))
     o.keep = (lr_dev, step_dev, grad_scale)
     for t, name, dtype in ((lr_dev, "lr_dev", torch.float32), (step_dev, "step_dev", torch.int64),
@@ -462,6 +474,7 @@ def haste_grad_norm_workspace_bytes(params) -> int:
 
 def haste_grad_norm(params, max_norm, out, ws=None, stream=None):
     """params: a param_list; out: two fp32 values on the GPU, the norm and the factor that clips it to max_norm."""
+    _list_here(params)
     p, n = _ws(ws)
     _check(lib.haste_grad_norm(params, len(params), max_norm, _vec(out, 2, "out", _here(out, "out")), p, n,
                                _stream(stream)))
@@ -469,6 +482,7 @@ def haste_grad_norm(params, max_norm, out, ws=None, stream=None):
 
 def haste_adamw(params, opts, stream=None):
     """One AdamW step over a param_list, in place."""
+    _list_here(params)
     _check(lib.haste_adamw(params, len(params), ctypes.byref(opts), _stream(stream)))
 
 

@@ -653,7 +653,9 @@ static int check_norm(int64_t B, int64_t F, int32_t dtype_a, int32_t dtype_b) {
     for (int32_t t : {dtype_a, dtype_b})
         if (t != HASTE_DTYPE_F32 && t != HASTE_DTYPE_BF16) return fail(HASTE_ERR_INVALID, "bad dtype %d", t);
     if (B < 0 || B > INT32_MAX) return fail(HASTE_ERR_INVALID, "B must be in [0, 2^31)");
-    if (F < 1 || F > INT32_MAX) return fail(HASTE_ERR_INVALID, "F must be in [1, 2^31)");
+    if (F < 1) return fail(HASTE_ERR_INVALID, "F must be >= 1");
+    if (F > haste::kNormWidthMax)      // as many as fp32 counts
+        return fail(HASTE_ERR_UNSUPPORTED, "F = %lld exceeds the supported maximum 2^24", (long long)F);
     return HASTE_OK;
 }
 

@@ -516,10 +516,11 @@ int64_t adamw_repeated(const haste_param_t *p, int64_t n) {
     return -1;
 }
 
-// Gradients and moments are not used again before the next step and go past the caches, so do weights that the
-// memory-side cache could not hold; others stay there for the next forward pass (58M fp32 weights: 274 us past the
-// caches, 236 through them; 239M bf16 weights with 8-bit moments: 460 and 484).
-constexpr int64_t kKeepBytes = (int64_t)256 << 20;
+// Gradients and moments are not used again before the next step and go past the caches.  So do weights, but for
+// lists that half of the memory-side cache holds: those go through it, and the next forward pass finds them there (58M
+// bf16 weights of three models in turn, fp32 moments: 238 us either way, and with a read of the weights behind it 284
+// us past the caches, 274 through them; 8-bit moments 165 and 158.  233 MB of fp32 weights: 365 either way).
+constexpr int64_t kKeepBytes = (int64_t)128 << 20;
 
 hipError_t adamw(const haste_param_t *p, int64_t n, const haste_adamw_opts_t &o, hipStream_t s) {
     StepList l;

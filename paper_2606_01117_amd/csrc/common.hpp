@@ -326,6 +326,7 @@ hipError_t fwd_bce_sgd_mfma(const TailArgs &a, const void *X, const int32_t *idx
 hipError_t sgd_momentum(int64_t n, int32_t dtype, const void *W, const float *g, float *m, const haste_sgd_t &opt,
                         void *W_next, hipStream_t s);
 // layer norm of rows; dweight and dbias (either may be NULL) through partial sums in ws (ln_bwd_ws)
+constexpr int64_t kNormWidthMax = (int64_t)1 << 24;
 hipError_t ln_fwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t ldh, const float *weight,
                   const float *bias, float eps, int32_t dtype_x, void *X, int64_t ldx, float *mean, float *rstd,
                   hipStream_t s);

@@ -650,6 +650,8 @@ hipError_t ln_bwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t 
             });
         });
     });
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
     if (wg && !few)
         hipLaunchKernelGGL(k_ln_wsum, dim3((unsigned)cdiv(2 * F, kWave)), dim3(1024), 0, s, part, parts, F, dweight, dbias, beta);
     return hipGetLastError();
