@@ -63,9 +63,7 @@ def _store(x, d, root):
     e = np.where(top > 0, np.frexp(np.where(top > 0, top, 1.0))[1] - 1 + 127, 0)
     s = np.maximum(e, 23) - 7
     y = fin * 2.0 ** (127.0 - s)[:, None]
-    # the stored magnitude lies on a grid of 2^-20 of E4M3's smallest step below it: fp32's, scaled
     small = y < 2.0 ** -6
-    y = np.where(small, np.rint(y * 2.0 ** 29) * 2.0 ** -29, y)
     step = np.where(small, 2.0 ** -9, 2.0 ** (np.floor(np.log2(np.where(small, 1.0, y))) - 3))
     q = np.floor(y / step + _blocks(d.astype(np.float64)) / 65536.0) * step
     if root:
