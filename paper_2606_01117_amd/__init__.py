@@ -335,7 +335,7 @@ def _vec(t, n, name, device):
     """Address of a contiguous fp32 vector of n values."""
     if t is None:
         return None
-    if t.numel() != n or t.dtype is not _torch().float32 or not t.is_contiguous():
+    if t.numel() != n or t.element_size() != 4 or not t.is_floating_point() or not t.is_contiguous():
         raise ValueError(f"{name} must be {n} contiguous fp32 values, got {tuple(t.shape)} {t.dtype}")
     if t.get_device() != device:
         _elsewhere(t, name)

@@ -545,8 +545,8 @@ void with_bwd_team(int64_t width, F &&f) {
 }
 
 // The backward kernel's workgroups.  Each leaves one row of sums, so there are no more than CUs, and a CU's rows
-// share its workgroup's teams, up to 1024 threads, about two rows a team at least (4099 x 1003 fp32 in up to 1024
-// workgroups of 256 threads, a row a team: 20.3 us, so 16.9).
+// share its workgroup's teams, up to 1024 threads, about four rows a team at least (one, two or four rows a team are
+// alike, 4099 x 1003 fp32 16.9 to 16.3 us; in up to 1024 workgroups of a row a team 20.3).
 struct BwdShape {
     int threads;
     int64_t blocks;
@@ -554,7 +554,7 @@ struct BwdShape {
 BwdShape bwd_shape(int64_t B, int64_t F) {
     const int team = bwd_team(F);
     int threads = team > 256 ? team : 256;
-    while (threads < 1024 && B > (int64_t)256 * 2 * (threads / team)) threads *= 2;
+    while (threads < 1024 && B > (int64_t)256 * 4 * (threads / team)) threads *= 2;
     const int64_t want = haste::cdiv(B, threads / team);
     return {threads, want < 256 ? want : 256};
 }
