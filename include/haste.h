@@ -392,7 +392,7 @@ int haste_head_bwd(int64_t B, int64_t F_s, int64_t H, int32_t dtype, const void 
  * elements only.  weight[F], bias[F] fp32 or NULL (ones, zeros).  mean[B], rstd[B] fp32, both or neither
  * (NULL): what haste_layer_norm_bwd takes.  X may be H where type and stride are the same.
  * Arithmetic: fp32, the squares around the row's mean; a bf16 X is rounded once.  An infinity or a NaN
- * makes its own row NaN.  eps >= 0; at 0 a row of equal values is NaN.  1 <= F <= 2^24; B < 2^31,
+ * makes its own row NaN.  X must not overlap H in any other way.  eps >= 0; at 0 a row of equal values is NaN.  1 <= F <= 2^24; B < 2^31,
  * B == 0 launches nothing.
  */
 int haste_layer_norm_fwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t ldh,
@@ -406,8 +406,8 @@ int haste_layer_norm_fwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, i
  *   dweight[f] = beta * dweight[f] + sum_b dX[b, f] * xh[b, f]
  *   dbias[f]   = beta * dbias[f] + sum_b dX[b, f]
  * dX (dtype_dx: the layer's own is fp32) and dH (dtype_h, overwritten) are rows lddx and lddh values apart,
- * H, ldh, weight, mean and rstd as in the forward call.  dH may be dX where type and stride are the same, and
- * NULL to skip it; dweight[F] and dbias[F] fp32, each NULL to skip it; beta is 0 (overwrite) or 1
+ * H, ldh, weight, mean and rstd as in the forward call.  dH may be dX where type and stride are the same (and
+ * overlap nothing in any other way), and NULL to skip it; dweight[F] and dbias[F] fp32, each NULL to skip it; beta is 0 (overwrite) or 1
  * (accumulate).
  * Sums are fp32; those over rows are formed in parts, in ws, and added in a fixed order.
  * ws: haste_layer_norm_workspace_bytes(B, F) bytes, where dweight or dbias is asked for.
