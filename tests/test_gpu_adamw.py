@@ -178,6 +178,65 @@ def test_mixed_list_with_empty_tensors(hs, bits):
             ref.adamw = plain
 
 
+@pytest.mark.parametrize("w,g,bits,master", [("f32", "f32", 32, False), ("bf16", "f32", 32, False), ("bf16", "bf16", 32, True),
+                                             ("f32", "bf16", 8, False), ("bf16", "bf16", 8, False), ("bf16", "f32", 8, True)])
+def test_long_lists_give_the_same_bits(hs, w, g, bits, master):
+    """Lists of more than 128 MB of weights take the accesses past the caches: the same tensors behind a large one and
+    behind an empty one of the same number."""
+    import torch
+    n = 70_000_000
+    z = lambda dt: torch.zeros(n, dtype=dt, device="cuda")
+    big = hs.param(z(torch.bfloat16), z(torch.bfloat16), z(torch.uint8), z(torch.uint8),
+                   torch.zeros((n + 31) // 32, 2, dtype=torch.uint8, device="cuda"))
+    got = []
+    for head in (hs.haste_param_t(n=0), big):
+        t = Tensors(hs, [1000, 33, 2048, 5], w, g, bits, master, edge=True)
+        before = t.snapshot()
+        hs.haste_adamw(hs.param_list([head, *t.params]), hs.adamw_opts(**OPTS))
+        torch.cuda.synchronize()
+        assert not torch.equal(before["W"], t.W)
+        got.append(t.snapshot())
+    assert all(torch.equal(got[0][k], got[1][k]) for k in got[0])
+    assert not bool(big.keep[0].any()) and not bool(big.keep[2].any()) and not bool(big.keep[3].any())
+
+
+def test_offsets_past_32_bits(hs):
+    """A tensor of more than 2^32 values: the step and the norm reach its end, its moments and draws go by the place."""
+    import torch
+    n = (1 << 32) + 32 * 7 + 5
+    W, G = (torch.zeros(n, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    m, v = (torch.zeros(n, dtype=torch.uint8, device="cuda") for _ in range(2))
+    scale = torch.zeros(((n + 31) // 32, 2), dtype=torch.uint8, device="cuda")
+    places = [0, 1 << 31, (1 << 32) - 64, (1 << 32) + 32 * 6]
+    ends = [p + 64 for p in places[:3]] + [n]
+    for p, e in zip(places, ends):
+        G[p:e] = torch.randn(e - p, device="cuda").bfloat16()
+        W[p:e] = torch.randn(e - p, device="cuda").bfloat16()
+    params = hs.param_list([hs.param(W, G, m, v, scale, weight_decay=0.1)])
+    old = [_np(W[p:e]) for p, e in zip(places, ends)]
+    out = torch.zeros(2, device="cuda")
+    hs.haste_grad_norm(params, 1e9, out, hs.workspace(hs.haste_grad_norm_workspace_bytes(params)))
+    hs.haste_adamw(params, hs.adamw_opts(**OPTS))
+    torch.cuda.synchronize()
+    total = math.sqrt(sum(float((G[p:e].double() ** 2).sum()) for p, e in zip(places, ends)))
+    assert abs(float(out[0]) - total) <= 1.01 * U * total
+    for p, e, w in zip(places, ends, old):
+        zero = np.zeros(e - p, np.uint8)
+        new, step, rm, rv, rs = ref.adamw(w, _np(G[p:e]), zero, zero, np.zeros(((e - p + 31) // 32, 2), np.uint8), OPTS, 0, 1.0,
+                                          0.1, 1.0, p)
+        np.testing.assert_array_equal(_np(m[p:e]), rm)
+        np.testing.assert_array_equal(_np(v[p:e]), rv)
+        np.testing.assert_array_equal(_np(scale[p // 32:(e + 31) // 32]), rs)
+        tol = 8 * U * step + 2 * U * np.abs(new)
+        assert np.all(np.abs(_np(W[p:e]) - new) <= tol * (1 + ref.U16) + ref.U16 * np.abs(new))
+    for lo in range(0, n, 1 << 30):               # the rest stays zero
+        hi = min(n, lo + (1 << 30))
+        rest = torch.ones(hi - lo, dtype=torch.bool, device="cuda")
+        for p, e in zip(places, ends):
+            rest[max(p - lo, 0):max(e - lo, 0)] = False
+        assert not bool((m[lo:hi] != 0)[rest].any()) and not bool((W[lo:hi] != 0)[rest].any())
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_options_on_the_device_and_the_factor(hs, bits):
     import torch
@@ -376,6 +435,7 @@ def _norm(hs, grads, max_norm, stream=None):
 
 
 @pytest.mark.parametrize("sizes", [[1], [0, 3, 0], [8191, 8192, 8193], [100003, 1], [1 + 53 * k % 999 for k in range(150)],
+                                   [1 + 71 * k % 501 for k in range(400)],
                                    [3_000_001, 70_000], [255, 256, 257, 1023, 1025, 16385, 32769, 65537]])
 @pytest.mark.parametrize("dt", ["f32", "bf16", "both"])
 def test_norm(hs, sizes, dt):

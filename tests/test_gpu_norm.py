@@ -141,6 +141,14 @@ def test_forward_and_backward(hs, B, F, h, x):
     c.check_backward(mean, rstd, *c.backward(hs, mean, rstd))
 
 
+@pytest.mark.parametrize("B,F", [(20000, 128), (20001, 131), (9000, 768), (8999, 769), (5000, 500), (3000, 2048), (2999, 1027),
+                                 (2500, 4096), (2100, 2051), (1300, 8192)])
+@pytest.mark.parametrize("h,x", [("bf16", "f32"), ("f32", "bf16")])
+def test_many_rows(hs, B, F, h, x):
+    """Workgroups of several teams, each of several rows."""
+    test_forward_and_backward(hs, B, F, h, x)
+
+
 @pytest.mark.parametrize("B,F,h,x,kw", [
     (12, 768, "f32", "bf16", dict(rows=5)), (12, 768, "bf16", "f32", dict(rows=3, first=768)),
     (9, 768, "bf16", "bf16", dict(first=1, pad=1)), (9, 768, "f32", "f32", dict(first=3, pad=5)),

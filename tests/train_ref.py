@@ -76,10 +76,10 @@ def _store(x, d, root):
     return code.astype(np.uint8), s.astype(np.uint8)
 
 
-def adamw(w, g, m, v, scale, o, k=0, lr_scale=1.0, decay=0.0, gs=1.0):
+def adamw(w, g, m, v, scale, o, k=0, lr_scale=1.0, decay=0.0, gs=1.0, first=0):
     """One step on fp32 arrays w (the weights before their rounding), g, m, v; scale is None or the 8-bit
-    moments' scales [blocks, 2] with m, v their bytes.  o: the options as a dict.  Returns (w in 64 bits, the
-    size of its update, m, v, scale)."""
+    moments' scales [blocks, 2] with m, v their bytes.  o: the options as a dict; first: the place of w[0] in
+    tensor k of the list, a multiple of 32.  Returns (w in 64 bits, the size of its update, m, v, scale)."""
     f32 = np.float32
     n = len(w)
     with np.errstate(all="ignore"):
@@ -101,7 +101,7 @@ def adamw(w, g, m, v, scale, o, k=0, lr_scale=1.0, decay=0.0, gs=1.0):
         step = lr * (decay * w + u)
         if scale is None:
             return w - step, np.abs(lr * u) + np.abs(lr * decay * w), m, v, None
-        i = np.arange(n, dtype=np.uint64)
+        i = np.arange(first, first + n, dtype=np.uint64)
         z = splitmix64(int(splitmix64(o["seed"] + t, 0)), (np.uint64(k) << np.uint64(40)) + (i >> np.uint64(2)))
         d = ((z >> (np.uint64(16) * (i & np.uint64(3)))) & np.uint64(0xffff)).astype(np.int64)
         qm, em = _store(m, d, False)
