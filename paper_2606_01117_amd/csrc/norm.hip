@@ -590,8 +590,10 @@ hipError_t ln_fwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t 
                 return;
             }
             with_fwd_team(F, [&](auto team, auto nc) {
+                // 16 waves a CU, which are all there at once, and 32 of teams that wait for each other (65536 x 768
+                // bf16 38.9 us with 16, 40.2 with 32; 8192 x 8192 63.7 and 51.8)
                 const int threads = team > 256 ? (int)team : 256;
-                const int64_t want = cdiv(B, threads / team), most = 256 * (2048 / threads);
+                const int64_t want = cdiv(B, threads / team), most = team > 256 ? 512 : 1024;
                 hipLaunchKernelGGL((k_ln_fwd<TH, TX, team, nc>), dim3((unsigned)(want < most ? want : most)), dim3(threads), 0,
                                    s, B, (int)F, (const TH *)H, ldh, weight, bias, eps, (TX *)X, ldx, mean, rstd);
             });
