@@ -27,14 +27,21 @@ __device__ __forceinline__ int tensor_of(const uint32_t (&start)[N], int count, 
 
 // ---- the norm ---------------------------------------------------------------------------------
 constexpr int kNormMax = 192;
-constexpr int64_t kNormChunk = 16384;
+
+// Values of a workgroup: enough to read ahead; of short lists one round of loads a thread, or they would run on a few
+// CUs (135K values: 4.4 us with 16384 a workgroup, 3.9 with 4096; 58M take 42 with 16384, 5.5 TB/s).
+int64_t norm_chunk(const haste_param_t *p, int64_t n) {
+    int64_t total = 0;
+    for (int64_t k = 0; k < n; ++k) total += p[k].n;
+    return total <= ((int64_t)1 << 22) ? 4096 : 16384;
+}
 
 struct NormList {
     const void *grad[kNormMax];
     int64_t n[kNormMax];
     uint32_t start[kNormMax];
     uint64_t bf16[kNormMax / 64];   // bit k: tensor k's gradient is bf16
-    int32_t count;
+    int32_t count, chunk;
 };
 static_assert(sizeof(NormList) <= 4096 - 16, "kernel arguments");
 
@@ -84,8 +91,8 @@ __device__ __forceinline__ double sum_squares(const T *g, int n) {
 __global__ __launch_bounds__(kThreads) void k_gn_part(NormList l, double *__restrict__ part) {
     __shared__ double red[kThreads / kWave];
     const int k = tensor_of<kNormMax>(l.start, l.count, blockIdx.x);
-    const int64_t i0 = (int64_t)(blockIdx.x - l.start[k]) * kNormChunk;
-    const int n = (int)(l.n[k] - i0 < kNormChunk ? l.n[k] - i0 : kNormChunk);
+    const int64_t i0 = (int64_t)(blockIdx.x - l.start[k]) * l.chunk;
+    const int n = (int)(l.n[k] - i0 < l.chunk ? l.n[k] - i0 : l.chunk);
     const double s = block_sum((l.bf16[k / 64] >> (k % 64)) & 1 ? sum_squares((const bf16_t *)l.grad[k] + i0, n)
                                                                 : sum_squares((const float *)l.grad[k] + i0, n), red);
     if (threadIdx.x == 0) part[blockIdx.x] = s;
@@ -461,21 +468,24 @@ static_assert(haste::kParamValuesMax / kChunk <= kMaxGrid, "one launch");
 namespace haste {
 
 size_t grad_norm_ws(const haste_param_t *p, int64_t n) {
+    const int64_t chunk = norm_chunk(p, n);
     int64_t parts = 0;
-    for (int64_t k = 0; k < n; ++k) parts += cdiv(p[k].n, kNormChunk);
+    for (int64_t k = 0; k < n; ++k) parts += cdiv(p[k].n, chunk);
     return (size_t)(parts > 0 ? parts : 1) * 8;
 }
 
 hipError_t grad_norm(const haste_param_t *p, int64_t n, float max_norm, float *out, void *ws, hipStream_t s) {
     double *part = (double *)ws;
     int64_t parts = 0;
+    const int64_t chunk = norm_chunk(p, n);
     NormList l;
+    l.chunk = (int32_t)chunk;
     l.count = 0;
     l.bf16[0] = l.bf16[1] = l.bf16[2] = 0;
     int64_t grid = 0;
     for (int64_t k = 0; k <= n; ++k) {
         if (k < n && p[k].n == 0) continue;
-        const int64_t c = k < n ? cdiv(p[k].n, kNormChunk) : 0;
+        const int64_t c = k < n ? cdiv(p[k].n, chunk) : 0;
         if (l.count > 0 && (k == n || l.count == kNormMax || grid + c > kMaxGrid)) {
             hipLaunchKernelGGL(k_gn_part, dim3((unsigned)grid), dim3(kThreads), 0, s, l, part + parts);
             const hipError_t e = hipGetLastError();
@@ -524,8 +534,9 @@ int64_t adamw_repeated(const haste_param_t *p, int64_t n) {
 
 // Gradients and moments are not used again before the next step and go past the caches.  So do weights, but for
 // lists that half of the memory-side cache holds: those go through it, and the next forward pass finds them there (58M
-// bf16 weights of three models in turn, fp32 moments: 238 us either way, and with a read of the weights behind it 284
-// us past the caches, 274 through them; 8-bit moments 165 and 158.  233 MB of fp32 weights: 365 either way).
+// bf16 weights, the step and a read of the weights behind it, past the caches and through them: 257 and 241 us with fp32
+// moments, 350 and 319 with fp32 copies too, 155 and 147 with 8-bit moments.  The step alone, where three models take
+// turns and none finds its weights: 238 either way, 299 and 314, 127 and 128.  233 MB of fp32 weights: 365 either way).
 constexpr int64_t kKeepBytes = (int64_t)128 << 20;
 
 hipError_t adamw(const haste_param_t *p, int64_t n, const haste_adamw_opts_t &o, hipStream_t s) {
