@@ -91,7 +91,7 @@ typedef struct haste_param {
 typedef struct haste_adamw_opts {
     double lr;              /* learning rate (finite, >= 0)                                       */
     double beta1, beta2;    /* decay of the moments, in [0, 1)                                    */
-    double eps;             /* added to the root of the second moment (>= 1.2e-38)                 */
+    double eps;             /* added to the root of the second moment (>= 1.2e-38)                */
     int64_t step;           /* number of this step, from 1                                        */
     uint64_t seed;          /* of the random bits that 8-bit moments are rounded with             */
     const float *lr_dev;       /* NULL, or a DEVICE value that takes the place of lr              */
@@ -391,9 +391,10 @@ int haste_head_bwd(int64_t B, int64_t F_s, int64_t H, int32_t dtype, const void 
  * next (>= F: the first tokens of sequences are rows of one sequence's length times F), aligned to their
  * elements only.  weight[F], bias[F] fp32 or NULL (ones, zeros).  mean[B], rstd[B] fp32, both or neither
  * (NULL): what haste_layer_norm_bwd takes.  X may be H where type and stride are the same.
+ * X must not overlap H in any other way.
  * Arithmetic: fp32, the squares around the row's mean; a bf16 X is rounded once.  An infinity or a NaN
- * makes its own row NaN.  X must not overlap H in any other way.  eps >= 0; at 0 a row of equal values is NaN.  1 <= F <= 2^24; B < 2^31,
- * B == 0 launches nothing.
+ * makes its own row NaN.  eps >= 0; at 0 a row of equal values is NaN.  1 <= F <= 2^24; B < 2^31, B == 0
+ * launches nothing.
  */
 int haste_layer_norm_fwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t ldh,
                          const float *weight, const float *bias, float eps, int32_t dtype_x, void *X,
@@ -406,10 +407,11 @@ int haste_layer_norm_fwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, i
  *   dweight[f] = beta * dweight[f] + sum_b dX[b, f] * xh[b, f]
  *   dbias[f]   = beta * dbias[f] + sum_b dX[b, f]
  * dX (dtype_dx: the layer's own is fp32) and dH (dtype_h, overwritten) are rows lddx and lddh values apart,
- * H, ldh, weight, mean and rstd as in the forward call.  dH may be dX where type and stride are the same (and
- * overlap nothing in any other way), and NULL to skip it; dweight[F] and dbias[F] fp32, each NULL to skip it; beta is 0 (overwrite) or 1
- * (accumulate).
- * Sums are fp32; those over rows are formed in parts, in ws, and added in a fixed order.
+ * H, ldh, weight, mean and rstd as in the forward call.  dH may be dX where type and stride are the same (it
+ * must not overlap H or dX in any other way), and NULL to skip it; dweight[F] and dbias[F] fp32, each NULL to skip
+ * it; beta is 0 (overwrite) or 1 (accumulate).
+ * Sums are fp32; those over rows are formed in parts, in ws, and added in a fixed order (up to 512 rows in another
+ * one where dH is dX).
  * ws: haste_layer_norm_workspace_bytes(B, F) bytes, where dweight or dbias is asked for.
  */
 int haste_layer_norm_bwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t ldh,
@@ -466,8 +468,8 @@ size_t haste_grad_norm_workspace_bytes(const haste_param_t *params, int64_t n_pa
  * Where *grad_scale is an infinity or a NaN, the call changes nothing: a step whose gradients overflowed is
  * passed over.  lr_dev, step_dev and grad_scale are read when the kernels run, so that a captured graph
  * follows them.  With step_dev no more than the value is read: the caller counts.
- * The arrays of the list must not overlap, but that gradients are only read (the same array twice is
- * refused).  No workspace.  At most 2^16 tensors of up to 2^33 values.
+ * Arrays that are updated must overlap nothing else that the call reads or updates (the same one twice is
+ * refused); gradients may be shared.  No workspace.  At most 2^16 tensors of up to 2^33 values.
  */
 int haste_adamw(const haste_param_t *params, int64_t n_params, const haste_adamw_opts_t *opts, void *stream);
 

@@ -317,11 +317,18 @@ def haste_head_bwd(B, F_s, H, dtype, X, W_head, dY_h, dW_h, dX, beta_dx=0, ws=No
                               int(beta_dx), p, n, _stream(stream)))
 
 
+_row_dtypes = {}
+
+
 def _rows(t, B, F, dtype, name):
     """Address and row stride of a [B, F] tensor whose rows may lie apart."""
     if t is None:
         return None, F
-    if t.shape != (B, F) or t.element_size() != (2 if dtype == HASTE_DTYPE_BF16 else 4):
+    if not _row_dtypes:
+        torch = _torch()
+        _row_dtypes.update({HASTE_DTYPE_F32: (torch.float32, torch.int32),        # the values, or their bits
+                            HASTE_DTYPE_BF16: (torch.bfloat16, torch.int16)})
+    if t.shape != (B, F) or t.dtype not in _row_dtypes.get(dtype, ()):
         raise ValueError(f"{name} must be [{B}, {F}] of the dtype that the call names, got {tuple(t.shape)} {t.dtype}")
     ld, step = t.stride()
     if F > 1 and step != 1:

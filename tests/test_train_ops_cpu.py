@@ -159,6 +159,9 @@ def test_binding_refuses_host_tensors(hs):
         hs.haste_layer_norm_fwd(4, 8, F32, x, None, None, 1e-5, F32, x)
     with pytest.raises(ValueError, match=r"\[4, 9\]"):
         hs.haste_layer_norm_fwd(4, 9, F32, x, None, None, 1e-5, F32, x)
+    for bad in (torch.float16, torch.float64, torch.bfloat16):
+        with pytest.raises(ValueError, match="dtype"):
+            hs.haste_layer_norm_fwd(4, 8, F32 if bad == torch.bfloat16 else BF16, x.to(bad), None, None, 1e-5, F32, x)
     with pytest.raises(ValueError, match="next to each other"):
         hs.haste_layer_norm_fwd(8, 4, F32, x.t(), None, None, 1e-5, F32, x)
     with pytest.raises(ValueError, match="overlap"):
