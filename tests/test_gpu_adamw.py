@@ -131,6 +131,7 @@ class Tensors:
 def _step(hs, t, opts, stream=None, **dev):
     import torch
     before = t.snapshot()
+    torch.cuda.synchronize()                     # the call may go to another stream
     hs.haste_adamw(t.params, hs.adamw_opts(**opts, **dev), stream)
     torch.cuda.synchronize()
     return before
@@ -387,7 +388,8 @@ def test_other_stream_and_repeat(hs, bits):
 def test_captured_norm_and_step_follow_device_options(hs, bits):
     """The norm's factor feeds the step inside one graph; the step's number is counted in it too."""
     import torch
-    t, e = (Tensors(hs, [3000, 17, 64], "bf16", "f32", bits, True) for _ in range(2))
+    # more tensors than one launch takes
+    t, e = (Tensors(hs, [3000, 17, 64] * 30, "bf16", "f32", bits, True) for _ in range(2))
     steps = [torch.zeros(1, dtype=torch.int64, device="cuda") for _ in range(2)]
     lr = torch.full((1,), 1e-2, device="cuda")
     outs = [torch.zeros(2, device="cuda") for _ in range(2)]
@@ -429,7 +431,9 @@ def _norm(hs, grads, max_norm, stream=None):
     import torch
     p = hs.param_list([hs.param(grad=g) for g in grads])
     out = torch.full((2,), -1.0, device="cuda")
-    hs.haste_grad_norm(p, max_norm, out, hs.workspace(hs.haste_grad_norm_workspace_bytes(p)), stream)
+    ws = hs.workspace(hs.haste_grad_norm_workspace_bytes(p))
+    torch.cuda.synchronize()                     # the call may go to another stream
+    hs.haste_grad_norm(p, max_norm, out, ws, stream)
     torch.cuda.synchronize()
     return [float(x) for x in out.cpu()]
 

@@ -68,6 +68,8 @@ class Case:
         import torch
         X = torch.full((self.B, self.F), 7.0, dtype=_dt(self.x), device="cuda") if X is None else X
         mean, rstd = (torch.full((self.B,), 7.0, device="cuda") if stats else None for _ in range(2))
+        if stream is not None:
+            torch.cuda.synchronize()
         hs.haste_layer_norm_fwd(self.B, self.F, _code(hs, self.h), self.H, self.w, self.b, self.eps, _code(hs, self.x), X,
                                 mean, rstd, stream)
         return X, mean, rstd
@@ -98,13 +100,15 @@ class Case:
         _, mu, rs = ref.layer_norm(_host(self.H), None, None, self.eps)
         return torch.from_numpy(mu[:, 0]).float().cuda(), torch.from_numpy(rs[:, 0]).float().cuda()
 
-    def backward(self, hs, mean, rstd, dH="new", dw="new", db="new", beta=0, stream=None, dX=None, ws=None):
+    def backward(self, hs, mean, rstd, dH="new", dw="new", db="new", beta=0, stream=None, dX=None, ws=None, sync=True):
         import torch
         new = {"dH": lambda: torch.full((self.B, self.F), 7.0, dtype=_dt(self.h), device="cuda"),
                "dw": lambda: torch.full((self.F,), 0.5, device="cuda")}
         dH = new["dH"]() if isinstance(dH, str) else dH
         dw, db = (new["dw"]() if isinstance(t, str) else t for t in (dw, db))
         ws = hs.workspace(hs.haste_layer_norm_workspace_bytes(self.B, self.F)) if ws is None else ws
+        if stream is not None and sync:
+            torch.cuda.synchronize()
         hs.haste_layer_norm_bwd(self.B, self.F, _code(hs, self.h), self.H, self.w, mean, rstd, _code(hs, self.x),
                                 self.dX if dX is None else dX, dH, dw, db, beta, ws, stream)
         return dH, dw, db
@@ -165,6 +169,32 @@ def test_strides_alignment_and_no_weight(hs, B, F, h, x, kw):
     X, none, _ = c.forward(hs, stats=False)
     assert none is None
     c.check_forward(X, None, None)
+
+
+@pytest.mark.parametrize("F", [100, 768, 9001])
+def test_weight_or_bias_alone(hs, F):
+    for drop in ("w", "b"):
+        c = Case(11, F, "bf16", "f32")
+        setattr(c, drop, None)
+        c.check_forward(*c.forward(hs))
+        mean, rstd = c.stats()
+        c.check_backward(mean, rstd, *c.backward(hs, mean, rstd))
+
+
+def test_two_streams_at_once(hs):
+    """Calls that overlap, each with a workspace of its own."""
+    import torch
+    cases = [Case(3000 + 7 * k, 768, "bf16", "f32", seed=k) for k in range(4)]
+    stats = [c.stats() for c in cases]
+    alone = [c.backward(hs, *s) for c, s in zip(cases, stats)]
+    ws = [hs.workspace(hs.haste_layer_norm_workspace_bytes(c.B, c.F)) for c in cases]
+    out = [[torch.zeros_like(t) for t in a] for a in alone]
+    side = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    got = [c.backward(hs, *s, *o, stream=q, ws=w, sync=False) for c, s, o, q, w in zip(cases, stats, out, side, ws)]
+    torch.cuda.synchronize()
+    for a, b in zip(alone, got):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
 
 
 @pytest.mark.parametrize("B,F", [(33, 768), (5, 99), (3, 4104), (2, 9001)])
