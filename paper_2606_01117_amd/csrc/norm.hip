@@ -233,8 +233,9 @@ __device__ __forceinline__ void bwd_rows(const Bwd<TH, TD> &a, int64_t b0, int64
         mu_next = a.mean[k];
         rs_next = a.rstd[k];
     };
-    // a row's values are asked for before the row before it is summed, where 128 registers a thread hold both
-    constexpr bool EARLY = !WG || NC < 4;
+    // a row's values are asked for before the row before it is summed, where the registers of 1024 threads, or of 512
+    // (bwd_threads), hold both
+    constexpr bool EARLY = TEAM == 1024 ? NC < 3 : !WG || NC != 4;
     if (EARLY) ask(b0 + team);
     float w[NC][4];
 #pragma unroll
@@ -309,10 +310,13 @@ __device__ __forceinline__ void store_own(float *out, const Run &r, const float 
         if (j >= r.skip) out[r.at + j] = v[j];
 }
 
+// threads of a workgroup whose threads hold so many runs in registers
+constexpr int bwd_threads(int runs) { return runs > 4 ? 512 : 1024; }
+
 // Rows, and (part not NULL) part[workgroup][0][f] and part[workgroup][1][f], the workgroup's sums for dweight and
 // dbias: its teams' terms, added in LDS run by run.
 template <typename TH, typename TD, int TEAM, int NC, bool STREAM>
-__global__ __launch_bounds__(1024) void k_ln_bwd(Bwd<TH, TD> a, float *__restrict__ part) {
+__global__ __launch_bounds__(bwd_threads(NC)) void k_ln_bwd(Bwd<TH, TD> a, float *__restrict__ part) {
     extern __shared__ float4 lds[];             // [teams][runs]
     const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM, teams = blockDim.x / TEAM, F = a.F;
     float aw[NC][4], ab[NC][4];
@@ -350,9 +354,10 @@ __global__ __launch_bounds__(1024) void k_ln_bwd(Bwd<TH, TD> a, float *__restric
 // Few rows, dH not in dX's place: one launch.  The workgroups from row_blocks on take eight columns each, straight
 // to dweight and dbias, every thread of a column blockDim / 8 rows apart.
 template <typename TH, typename TD, int TEAM, int NC>
-__global__ __launch_bounds__(1024) void k_ln_bwd_few(Bwd<TH, TD> a, unsigned row_blocks, float *__restrict__ dweight,
+__global__ __launch_bounds__(TEAM > 256 ? TEAM : 256) void k_ln_bwd_few(Bwd<TH, TD> a, unsigned row_blocks, float *__restrict__ dweight,
                                                      float *__restrict__ dbias, int beta) {
-    __shared__ float sw[1024], sb[1024];
+    constexpr int T = TEAM > 256 ? TEAM : 256;
+    __shared__ float sw[T], sb[T];
     if (blockIdx.x < row_blocks) {
         const int teams = blockDim.x / TEAM;
         float aw[NC][4], ab[NC][4];
@@ -506,57 +511,61 @@ __global__ __launch_bounds__(kThreads) void k_ln_wgrad_wide(int64_t B, int64_t F
 }
 
 // ---- which team takes a row ---------------------------------------------------------------------------
-constexpr int64_t kWideF = 8192;       // rows beyond it are not held in registers
+constexpr int64_t kWideF = 16384;      // rows beyond it are not held in registers
 bool held(int64_t F) { return F >= 4 && F <= kWideF; }
 constexpr int kMaxRowBlocks = 65536;   // workgroups of the kernels for them; more rows go round
 
+// The team that holds a row in few registers a thread, forward and backward (which adds up terms in registers too).
 constexpr int fwd_team(int64_t F) { return F <= 256 ? 16 : F <= 1024 ? 64 : F <= 4096 ? 256 : 1024; }
 constexpr int bwd_team(int64_t F) { return F <= 256 ? 16 : F <= 1024 ? 64 : F <= 2048 ? 256 : F <= 4096 ? 512 : 1024; }
+int64_t runs_of(int64_t F, int team) { return haste::cdiv(F, 4 * team); }
 
-// f(team, runs of four values a thread), the team one of the constants that team_of gives up to kWideF
+// Where no more than three quarters of its runs were filled, a smaller team of up to six runs a thread takes bf16 rows
+// (39024 x 1025 bf16: forward 56 us and 37, backward 90 and 58; 8000 x 5000: 44 and 34, 69 and 50).  Rows of fp32 alone
+// are bound by memory with the runs half empty too, and slower in more registers (31250 x 1280: forward 58 and 61,
+// backward, where H's type decides, 91 and 100).
+int pick_team(int64_t F, int team, bool bf16) {
+    const int small = team == 1024 || team == 512 ? 256 : team == 256 ? 64 : 16;
+    return bf16 && team > 16 && 4 * F <= 3 * (4 * team * runs_of(F, team)) && runs_of(F, small) <= 6 ? small : team;
+}
+
+// f(team, runs of four values a thread), both as constants
 template <int LEAST, int MOST, typename F>
 void with_runs(int64_t n, F &&f) {
     if constexpr (LEAST < MOST)
         if (n > LEAST) return with_runs<LEAST + 1, MOST>(n, f);
     f(std::integral_constant<int, LEAST>{});
 }
-template <int TEAM, int MOST, typename F>
-void with_team(int64_t width, F &&f) {
-    with_runs<1, MOST>(haste::cdiv(width, 4 * TEAM), [&](auto nc) { f(std::integral_constant<int, TEAM>{}, nc); });
-}
 template <typename F>
-void with_fwd_team(int64_t width, F &&f) {
-    switch (fwd_team(width)) {
-    case 16: return with_team<16, 4>(width, f);
-    case 64: return with_team<64, 4>(width, f);
-    case 256: return with_team<256, 4>(width, f);
-    default: return with_team<1024, 2>(width, f);
-    }
-}
-template <typename F>
-void with_bwd_team(int64_t width, F &&f) {
-    switch (bwd_team(width)) {
-    case 16: return with_team<16, 4>(width, f);
-    case 64: return with_team<64, 4>(width, f);
-    case 256: return with_team<256, 2>(width, f);
-    case 512: return with_team<512, 2>(width, f);
-    default: return with_team<1024, 2>(width, f);
+void with_team(int team, int64_t width, F &&f) {
+    auto go = [&](auto t, auto least, auto most) {
+        with_runs<least, most>(runs_of(width, t), [&](auto nc) { f(t, nc); });
+    };
+    typedef std::integral_constant<int, 1> one;
+    typedef std::integral_constant<int, 2> two;
+    typedef std::integral_constant<int, 6> six;
+    switch (team) {
+    case 16: return go(std::integral_constant<int, 16>{}, one{}, six{});
+    case 64: return go(std::integral_constant<int, 64>{}, two{}, six{});
+    case 256: return go(std::integral_constant<int, 256>{}, two{}, six{});
+    case 512: return go(std::integral_constant<int, 512>{}, two{}, two{});
+    default: return go(std::integral_constant<int, 1024>{}, two{}, std::integral_constant<int, 4>{});
     }
 }
 
 // The backward kernel's workgroups.  Each leaves one row of sums, so there are no more than CUs, and a CU's rows
-// share its workgroup's teams, up to 1024 threads, about four rows a team at least (one, two or four rows a team are
-// alike, 4099 x 1003 fp32 16.9 to 16.3 us; in up to 1024 workgroups of a row a team 20.3).
+// share its workgroup's teams, up to bwd_threads of its registers, about four rows a team at least (one, two or four
+// rows a team are alike, 4099 x 1003 fp32 16.9 to 16.3 us; in up to 1024 workgroups of a row a team 20.3).
 struct BwdShape {
-    int threads;
+    int team, threads;
     int64_t blocks;
 };
-BwdShape bwd_shape(int64_t B, int64_t F) {
-    const int team = bwd_team(F);
+BwdShape bwd_shape(int64_t B, int64_t F, int32_t dtype_h) {
+    const int team = pick_team(F, bwd_team(F), dtype_h == HASTE_DTYPE_BF16), most = bwd_threads((int)runs_of(F, team));
     int threads = team > 256 ? team : 256;
-    while (threads < 1024 && B > (int64_t)256 * 4 * (threads / team)) threads *= 2;
+    while (threads < most && B > (int64_t)256 * 4 * (threads / team)) threads *= 2;
     const int64_t want = haste::cdiv(B, threads / team);
-    return {threads, want < 256 ? want : 256};
+    return {team, threads, want < 256 ? want : 256};
 }
 // Rows whose column sums a second pass over them, from the caches, forms as fast as partial sums would be added.
 constexpr int64_t kFewRows = 512;
@@ -589,7 +598,8 @@ hipError_t ln_fwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t 
                                    dim3(kThreads), 0, s, B, F, (const TH *)H, ldh, weight, bias, eps, (TX *)X, ldx, mean, rstd);
                 return;
             }
-            with_fwd_team(F, [&](auto team, auto nc) {
+            const bool bf16 = dtype_h == HASTE_DTYPE_BF16 || dtype_x == HASTE_DTYPE_BF16;
+            with_team(pick_team(F, fwd_team(F), bf16), F, [&](auto team, auto nc) {
                 // 16 waves a CU, which are all there at once, and 32 of teams that wait for each other (65536 x 768
                 // bf16 38.9 us with 16, 40.2 with 32; 8192 x 8192 63.7 and 51.8)
                 const int threads = team > 256 ? (int)team : 256;
@@ -603,7 +613,12 @@ hipError_t ln_fwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t 
 }
 
 size_t ln_bwd_ws(int64_t B, int64_t F) {
-    return (size_t)((!held(F) ? wide_parts(B) : bwd_shape(B, F).blocks) * 2 * F * 4);
+    int64_t parts = wide_parts(B);
+    if (held(F)) {
+        const int64_t a = bwd_shape(B, F, HASTE_DTYPE_F32).blocks, b = bwd_shape(B, F, HASTE_DTYPE_BF16).blocks;
+        parts = a > b ? a : b;
+    }
+    return (size_t)(parts * 2 * F * 4);
 }
 
 hipError_t ln_bwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t ldh, const float *weight,
@@ -611,7 +626,7 @@ hipError_t ln_bwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t 
                   int64_t lddh, float *dweight, float *dbias, int beta, void *ws, hipStream_t s) {
     float *part = (float *)ws;
     const bool wg = dweight || dbias;
-    const BwdShape n = bwd_shape(B, F);
+    const BwdShape n = held(F) ? bwd_shape(B, F, dtype_h) : BwdShape{};
     const int64_t parts = !held(F) ? wide_parts(B) : n.blocks;
     const bool few = wg && B <= kFewRows && held(F) && dH != dX;
     with_type(dtype_h, [&](auto th) {
@@ -635,7 +650,7 @@ hipError_t ln_bwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t 
             };
             const bool stream = whole(H, ldh, sizeof(TH)) && whole(dX, lddx, sizeof(TD));
             const Bwd<TH, TD> a = {B, (int)F, (const TH *)H, ldh, weight, mean, rstd, (const TD *)dX, lddx, (TH *)dH, lddh};
-            with_bwd_team(F, [&](auto team, auto nc) {
+            with_team(n.team, F, [&](auto team, auto nc) {
                 const int teams = n.threads / team;
                 const size_t lds = wg && teams > 1 ? (size_t)teams * cdiv(F, 4) * 16 : 0;
                 if (few) {

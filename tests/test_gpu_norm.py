@@ -132,7 +132,9 @@ class Case:
 
 
 SIZES = [(1, 1), (1, 768), (3, 2), (5, 63), (7, 64), (2, 65), (33, 100), (512, 768), (77, 500), (129, 1003), (40, 1024),
-         (17, 1030), (9, 2048), (6, 2049), (5, 4096), (3, 8191), (4, 8192), (2, 8200), (2, 20001), (1500, 96), (4100, 256)]
+         (17, 1030), (9, 2048), (6, 2049), (5, 4096), (3, 8191), (4, 8192), (2, 8200), (2, 20001), (1500, 96),
+         (4100, 256), (6, 300), (5, 384), (4, 385), (5, 1025), (4, 1300), (3, 1536), (3, 2500), (2, 4097), (2, 5000),
+         (2, 6144), (2, 9000), (2, 12289), (2, 16384), (2, 16385)]
 
 
 @pytest.mark.parametrize("B,F", SIZES)
@@ -145,8 +147,9 @@ def test_forward_and_backward(hs, B, F, h, x):
     c.check_backward(mean, rstd, *c.backward(hs, mean, rstd))
 
 
-@pytest.mark.parametrize("B,F", [(20000, 128), (20001, 131), (9000, 768), (8999, 769), (5000, 500), (3000, 2048), (2999, 1027),
-                                 (2500, 4096), (2100, 2051), (1300, 8192)])
+@pytest.mark.parametrize("B,F", [(20000, 128), (20001, 131), (9000, 768), (8999, 769), (5000, 500), (3000, 2048),
+                                 (2999, 1027), (2500, 4096), (2100, 2051), (1300, 8192), (20000, 301), (5000, 1026),
+                                 (4000, 1500), (2000, 5001), (700, 9001), (600, 16000)])
 @pytest.mark.parametrize("h,x", [("bf16", "f32"), ("f32", "bf16")])
 def test_many_rows(hs, B, F, h, x):
     """Workgroups of several teams, each of several rows."""
