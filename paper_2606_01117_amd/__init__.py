@@ -438,15 +438,43 @@ def param(W=None, grad=None, m=None, v=None, scale=None, W32=None, lr_scale=1.0,
     return p
 
 
+class _Entries:
+    """The array of a list's entries.  One that is taken out of it or put into it brings its tensors and their device
+    along: a ctypes array alone copies the addresses, and the tensors behind them could be freed."""
+
+    def __getitem__(self, k):
+        if isinstance(k, slice):
+            return [self[i] for i in range(*k.indices(len(self)))]
+        p = super().__getitem__(k)               # the entry in place: what is written to it, the list has
+        p.keep = self.keep[k]
+        p.device = None if p.keep is None else self.device
+        return p
+
+    def __setitem__(self, k, p):
+        if isinstance(k, slice):
+            raise TypeError("the entries of a list are set one by one")
+        device = getattr(p, "device", None)
+        if device is not None and self.device is not None and device != self.device:
+            raise ValueError(f"the tensors of a list must be on one GPU, not on {sorted((device, self.device))}")
+        super().__setitem__(k, p)
+        self.keep[k] = getattr(p, "keep", None)
+        self.device = device if self.device is None else self.device
+
+
+_list_types = {}
+
+
 def param_list(params):
-    """The array of entries that haste_grad_norm and haste_adamw take; made once, it serves every step."""
+    """The array of entries that haste_grad_norm and haste_adamw take; made once, it serves every step.  Entries may be
+    taken out of one list and put into another, or replaced in place."""
     params = list(params)
-    devices = {getattr(p, "device", None) for p in params} - {None}
-    if len(devices) > 1:
-        raise ValueError(f"the tensors of a list must be on one GPU, not on {sorted(devices)}")
-    array = (haste_param_t * len(params))(*params)
-    array.keep = [getattr(p, "keep", None) for p in params]
-    array.device = devices.pop() if devices else None
+    n = len(params)
+    if n not in _list_types:
+        _list_types[n] = type("param_list", (_Entries, haste_param_t * n), {})
+    array = _list_types[n]()
+    array.keep, array.device = [None] * n, None
+    for k, p in enumerate(params):
+        array[k] = p
     return array
 
 

@@ -1,0 +1,67 @@
+"""The binding's lists of tensors: what they keep alive, and what they and the calls refuse (no GPU needed)."""
+import gc
+import weakref
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def hs():
+    import paper_2606_01117_amd as m
+    return m
+
+
+class Thing:
+    """In a tensor's place, where only its life counts."""
+
+
+def _entry(hs, n=1, device=0):
+    p = hs.haste_param_t(n=n)
+    thing = Thing()
+    p.keep, p.device = (thing,), device
+    return p, weakref.ref(thing)
+
+
+def test_entries_taken_out_of_a_list_keep_their_tensors(hs):
+    (a, ra), (b, rb) = _entry(hs, 5), _entry(hs, 7)
+    first = hs.param_list([a, b])
+    second = hs.param_list([first[1], *first[:1]])
+    del a, b, first
+    gc.collect()
+    assert [p.n for p in second] == [7, 5]
+    assert ra() is not None and rb() is not None
+    del second
+    gc.collect()
+    assert ra() is None and rb() is None
+
+
+def test_an_entry_put_into_a_list_takes_its_tensors_along(hs):
+    (a, ra), (b, rb) = _entry(hs, 5), _entry(hs, 7)
+    params = hs.param_list([a])
+    params[0] = b
+    del a, b
+    gc.collect()
+    assert params[0].n == 7 and params[-1].n == 7 and rb() is not None
+    assert ra() is None, "nothing names it any more"
+    with pytest.raises(TypeError):
+        params[:] = [params[0]]
+
+
+def test_lists_know_their_device_wherever_their_entries_come_from(hs):
+    here, there = hs.param_list([_entry(hs, device=0)[0]]), hs.param_list([_entry(hs, device=1)[0]])
+    assert (here.device, there.device) == (0, 1)
+    assert hs.param_list(there[:]).device == 1
+    with pytest.raises(ValueError, match="one GPU"):
+        hs.param_list([here[0], there[0]])
+    with pytest.raises(ValueError, match="one GPU"):
+        here[0] = there[0]
+    empty = hs.param_list([hs.haste_param_t(n=0), here[0]])
+    assert empty.device == 0 and empty[0].device is None
+    assert len(hs.param_list([])) == 0
+
+
+def test_an_entry_written_in_place_is_the_lists(hs):
+    params = hs.param_list([hs.haste_param_t(n=3), hs.haste_param_t(n=4)])
+    params[1].weight_decay = 0.25
+    assert params[1].weight_decay == 0.25 and [p.n for p in params] == [3, 4]
+    assert hs.haste_grad_norm_workspace_bytes(params) > 0
