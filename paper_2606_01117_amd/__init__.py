@@ -465,8 +465,8 @@ _list_types = {}
 
 
 def param_list(params):
-    """The array of entries that haste_grad_norm and haste_adamw take; made once, it serves every step.  Entries may be
-    taken out of one list and put into another, or replaced in place."""
+    """The array of entries that haste_grad_norm and haste_adamw take; made once, it serves every step (set_grads points
+    it at new gradients).  Entries may be taken out of one list and put into another, or replaced in place."""
     params = list(params)
     n = len(params)
     if n not in _list_types:
@@ -476,6 +476,31 @@ def param_list(params):
     for k, p in enumerate(params):
         array[k] = p
     return array
+
+
+def set_grads(params, grads):
+    """Points a param_list at new gradients, in the order of its entries: contiguous, fp32 or bf16, of the entries' sizes,
+    on the list's GPU; None leaves an entry's gradient as it is.  The list keeps the new tensors alive and no longer the
+    old ones; nothing is changed where one of them is refused.  A graph captured before holds the old addresses."""
+    grads = list(grads)
+    if len(grads) != len(params):
+        raise ValueError(f"{len(grads)} gradients for a list of {len(params)} tensors")
+    entries, dtypes = params[:], [None if g is None else _dtype_of(g, "grad") for g in grads]
+    device = params.device
+    for k, (p, g) in enumerate(zip(entries, grads)):
+        if g is None:
+            continue
+        device = _here(g, "grad") if device is None else device
+        if g.numel() != p.n or not g.is_contiguous():
+            raise ValueError(f"grad of tensor {k} must be {p.n} contiguous values, got {tuple(g.shape)}")
+        if g.get_device() != device:
+            raise ValueError(f"grad of tensor {k} is on {g.device}, the list on cuda:{device}")
+    for k, (p, g, dtype) in enumerate(zip(entries, grads, dtypes)):
+        if g is not None:
+            p.grad, p.grad_dtype = g.data_ptr(), dtype
+            keep = params.keep[k] or (None,) * 6
+            params.keep[k] = (keep[0], g, *keep[2:])
+    params.device = device
 
 
 def _list_here(params):

@@ -65,3 +65,54 @@ def test_an_entry_written_in_place_is_the_lists(hs):
     params[1].weight_decay = 0.25
     assert params[1].weight_decay == 0.25 and [p.n for p in params] == [3, 4]
     assert hs.haste_grad_norm_workspace_bytes(params) > 0
+
+
+# ---- new gradients ------------------------------------------------------------------------------------
+@pytest.fixture
+def on_host(hs, monkeypatch):
+    """Lets the binding make lists of host tensors, for what it checks and keeps itself (their device is -1)."""
+    monkeypatch.setattr(hs, "_here", lambda t, name: t.get_device())
+
+
+def _host_list(hs, sizes=(5, 8), bits=32):
+    import torch
+    return hs.param_list([hs.param(torch.zeros(n), torch.ones(n), torch.zeros(n), torch.zeros(n)) for n in sizes])
+
+
+def test_new_gradients_are_kept_and_the_old_ones_let_go(hs, on_host):
+    import torch
+    params = _host_list(hs)
+    old, weights = [weakref.ref(p.keep[1]) for p in params], [p.W for p in params]
+    fresh = torch.full((2, 4), 2.0).bfloat16()
+    new = weakref.ref(fresh)
+    hs.set_grads(params, [None, fresh])
+    assert params[1].grad == fresh.data_ptr() and params[1].grad_dtype == hs.HASTE_DTYPE_BF16
+    assert params[0].grad_dtype == hs.HASTE_DTYPE_F32 and params[0].grad == old[0]().data_ptr()
+    del fresh
+    gc.collect()
+    assert new() is not None and old[0]() is not None and old[1]() is None
+    assert [p.W for p in params] == weights and all(t is not None for p in params for t in p.keep[:4])
+
+
+def test_new_gradients_that_do_not_fit_change_nothing(hs, on_host):
+    import torch
+    params = _host_list(hs)
+    before = [(p.grad, p.grad_dtype) for p in params]
+    good = torch.ones(5)
+    for bad, what in ((torch.ones(9), "8 contiguous"), (torch.ones(8, 2)[:, 0], "8 contiguous"), (torch.ones(8).half(), "float32")):
+        with pytest.raises(ValueError, match=what):
+            hs.set_grads(params, [good, bad])
+    params.device = 0                            # a list on a GPU takes no host tensor
+    with pytest.raises(ValueError, match="is on cpu, the list on cuda:0"):
+        hs.set_grads(params, [good, None])
+    with pytest.raises(ValueError, match="1 gradients for a list of 2"):
+        hs.set_grads(params, [good])
+    assert [(p.grad, p.grad_dtype) for p in params] == before
+
+
+def test_new_gradients_for_entries_without_tensors(hs, on_host):
+    import torch
+    params = hs.param_list([hs.haste_param_t(n=4)])
+    g = torch.ones(4)
+    hs.set_grads(params, [g])
+    assert params[0].grad == g.data_ptr() and params[0].keep[1] is g and params.device == -1
