@@ -425,7 +425,10 @@ def param(W=None, grad=None, m=None, v=None, scale=None, W32=None, lr_scale=1.0,
     if m is not None and v is not None:
         if m.element_size() == 1 and v.element_size() == 1:
             bits = 8
-            if scale is None or scale.element_size() != 1:
+            for t, name in ((m, "m"), (v, "v")):
+                if t.dtype not in (_torch().uint8, _torch().int8, _torch().float8_e4m3fn):    # bytes, or what they are
+                    raise ValueError(f"8-bit {name} must be uint8 or float8_e4m3fn, got {t.dtype}")
+            if scale is None or scale.dtype not in (_torch().uint8, _torch().int8, _torch().float8_e8m0fnu):
                 raise ValueError(f"8-bit moments of {n} values need scale, uint8 [{(n + 31) // 32}, 2]")
         elif _dtype_of(m, "m") != HASTE_DTYPE_F32 or _dtype_of(v, "v") != HASTE_DTYPE_F32:
             raise ValueError("m and v must both be torch.float32, or both of one byte a value")

@@ -116,3 +116,19 @@ def test_new_gradients_for_entries_without_tensors(hs, on_host):
     g = torch.ones(4)
     hs.set_grads(params, [g])
     assert params[0].grad == g.data_ptr() and params[0].keep[1] is g and params.device == -1
+
+
+# ---- entries ------------------------------------------------------------------------------------------
+def test_moments_of_other_8_bit_types_are_refused(hs, on_host):
+    """Those of E4M3 without negative zero and of E5M2, and truth values, would be taken for other values."""
+    import torch
+    x, q, s = torch.zeros(64), torch.zeros(64, dtype=torch.uint8), torch.zeros((2, 2), dtype=torch.uint8)
+    for good in (torch.uint8, torch.int8, torch.float8_e4m3fn):
+        for exponents in (torch.uint8, torch.int8, torch.float8_e8m0fnu):
+            assert hs.param(x, x, q.view(good), q.view(good), s.view(exponents)).state_bits == 8
+    for bad in (torch.float8_e4m3fnuz, torch.float8_e5m2, torch.float8_e5m2fnuz, torch.bool):
+        for m, v in ((q.view(bad), q), (q, q.view(bad))):
+            with pytest.raises(ValueError, match="must be uint8 or float8_e4m3fn"):
+                hs.param(x, x, m, v, s)
+    with pytest.raises(ValueError, match="need scale"):
+        hs.param(x, x, q, q, s.view(torch.float8_e4m3fn))
