@@ -351,6 +351,8 @@ def _vec(t, n, name, device):
 
 def _here(t, name):
     """The device of a tensor, which must be the current GPU."""
+    if t is None:
+        raise ValueError(f"{name} is missing")
     device = t.get_device()
     if device < 0 or device != _torch().cuda.current_device():
         _elsewhere(t, name)
@@ -371,6 +373,8 @@ def haste_layer_norm_fwd(B, F, dtype_h, H, weight, bias, eps, dtype_x, X, mean=N
     """H and X: [B, F] tensors of dtype_h and dtype_x; their rows may lie apart (a view such as tokens[:, 0])."""
     (h, ldh), (x, ldx) = _rows(H, B, F, dtype_h, "H"), _rows(X, B, F, dtype_x, "X")
     on = _here(H, "H")
+    if X is None:
+        raise ValueError("X is missing")
     if X.get_device() != on:
         _elsewhere(X, "X")
     _check(lib.haste_layer_norm_fwd(B, F, dtype_h, h, ldh, _vec(weight, F, "weight", on), _vec(bias, F, "bias", on), eps,
@@ -409,6 +413,8 @@ def param(W=None, grad=None, m=None, v=None, scale=None, W32=None, lr_scale=1.0,
     W (fp32 or bf16), grad (fp32 or bf16), and the moments m and v: fp32, or of one byte a value (uint8, or
     float8_e4m3fn) with scale, uint8 [ceil(n / 32), 2].  All contiguous, of n values each, on the current GPU.  The
     entry keeps the tensors alive."""
+    if grad is None and W is None:
+        raise ValueError("an entry needs grad, or W")
     first = grad if grad is not None else W
     n, device = first.numel(), _here(first, "grad" if grad is not None else "W")
 

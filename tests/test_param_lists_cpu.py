@@ -132,3 +132,21 @@ def test_moments_of_other_8_bit_types_are_refused(hs, on_host):
                 hs.param(x, x, m, v, s)
     with pytest.raises(ValueError, match="need scale"):
         hs.param(x, x, q, q, s.view(torch.float8_e4m3fn))
+
+
+def test_missing_tensors_are_named(hs, on_host, monkeypatch):
+    import torch
+    x, v = torch.zeros(4, 8), torch.zeros(4)
+    with pytest.raises(ValueError, match="needs grad, or W"):
+        hs.param()
+    monkeypatch.undo()
+    for H, X, name in ((None, x, "H"), (None, None, "H")):
+        with pytest.raises(ValueError, match=f"{name} is missing"):
+            hs.haste_layer_norm_fwd(4, 8, 0, H, None, None, 1e-5, 0, X)
+    with pytest.raises(ValueError, match="H is missing"):
+        hs.haste_layer_norm_bwd(4, 8, 0, None, None, v, v, 0, x)
+    with pytest.raises(ValueError, match="out is missing"):
+        hs.haste_grad_norm(hs.param_list([]), 1.0, None)
+    monkeypatch.setattr(hs, "_here", lambda t, name: -1)
+    with pytest.raises(ValueError, match="X is missing"):
+        hs.haste_layer_norm_fwd(4, 8, 0, x, None, None, 1e-5, 0, None)
