@@ -512,11 +512,11 @@ def set_grads(params, grads):
     params.device = device
 
 
-def _list_here(params):
-    device = getattr(params, "device", None)
+def _still_here(what, name):
+    """Tensors that a list or options hold must be on the GPU that is current at the call, too."""
+    device = getattr(what, "device", None)
     if device is not None and device != _torch().cuda.current_device():
-        raise ValueError(f"the list's tensors are on cuda:{device}, not on the current device "
-                         f"cuda:{_torch().cuda.current_device()}")
+        raise ValueError(f"{name} are on cuda:{device}, not on the current device cuda:{_torch().cuda.current_device()}")
 
 
 def adamw_opts(lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, seed=0, lr_dev=None, step_dev=None,
@@ -526,13 +526,14 @@ def adamw_opts(lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, seed=0, lr_dev=None
     torch = _torch()
     o = haste_adamw_opts_t(lr=lr, beta1=beta1, beta2=beta2, eps=eps, step=step, seed=seed & ((1 << 64) - 1))
     o.keep = (lr_dev, step_dev, grad_scale)
+    o.device = None
     for t, name, dtype in ((lr_dev, "lr_dev", torch.float32), (step_dev, "step_dev", torch.int64),
                            (grad_scale, "grad_scale", torch.float32)):
         if t is None:
             continue
         if t.numel() != 1 or t.dtype != dtype:
             raise ValueError(f"{name} must be one value of {dtype}")
-        _here(t, name)
+        o.device = _here(t, name)
         setattr(o, name, t.data_ptr())
     return o
 
@@ -543,7 +544,7 @@ def haste_grad_norm_workspace_bytes(params) -> int:
 
 def haste_grad_norm(params, max_norm, out, ws=None, stream=None):
     """params: a param_list; out: two fp32 values on the GPU, the norm and the factor that clips it to max_norm."""
-    _list_here(params)
+    _still_here(params, "the list's tensors")
     p, n = _ws(ws)
     _check(lib.haste_grad_norm(params, len(params), max_norm, _vec(out, 2, "out", _here(out, "out")), p, n,
                                _stream(stream)))
@@ -551,7 +552,8 @@ def haste_grad_norm(params, max_norm, out, ws=None, stream=None):
 
 def haste_adamw(params, opts, stream=None):
     """One AdamW step over a param_list, in place."""
-    _list_here(params)
+    _still_here(params, "the list's tensors")
+    _still_here(opts, "the options' tensors")
     _check(lib.haste_adamw(params, len(params), ctypes.byref(opts), _stream(stream)))
 
 

@@ -150,3 +150,22 @@ def test_missing_tensors_are_named(hs, on_host, monkeypatch):
     monkeypatch.setattr(hs, "_here", lambda t, name: -1)
     with pytest.raises(ValueError, match="X is missing"):
         hs.haste_layer_norm_fwd(4, 8, 0, x, None, None, 1e-5, 0, None)
+
+
+def test_options_and_lists_made_on_another_device_are_refused(hs, on_host, monkeypatch):
+    """Refused before the call: the lists are empty, and the options wrong, so that nothing could be launched."""
+    import torch
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(hs, "_here", lambda t, name: 0)
+    empty = hs.param_list([])
+    for name, dtype in (("lr_dev", torch.float32), ("step_dev", torch.int64), ("grad_scale", torch.float32)):
+        opts = hs.adamw_opts(1e-3, **{name: torch.zeros(1, dtype=dtype)})
+        with pytest.raises(ValueError, match="options' tensors are on cuda:0, not on the current device cuda:1"):
+            hs.haste_adamw(empty, opts)
+    opts = hs.adamw_opts(-1.0)                   # no tensors: the call itself refuses it
+    with pytest.raises(hs.HasteError, match="lr"):
+        hs.haste_adamw(empty, opts, stream=0)
+    empty.device = 0
+    for call in (lambda: hs.haste_adamw(empty, opts), lambda: hs.haste_grad_norm(empty, 1.0, torch.zeros(2))):
+        with pytest.raises(ValueError, match="list's tensors are on cuda:0"):
+            call()
