@@ -810,6 +810,7 @@ int haste_adamw(const haste_param_t *params, int64_t n_params, const haste_adamw
             return fail(HASTE_ERR_INVALID, "tensor %lld: scale is not 2-byte aligned", (long long)k);
     }
     const int64_t twice = haste::adamw_repeated(params, n_params);
+    if (twice == -2) return hip_status(hipErrorOutOfMemory, "haste_adamw");
     if (twice >= 0)
         return fail(HASTE_ERR_INVALID, "tensor %lld: an array that is updated occurs twice in the list", (long long)twice);
     return hip_status(haste::adamw(params, n_params, *opts, as_stream(stream)), "haste_adamw");

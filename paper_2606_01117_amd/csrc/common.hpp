@@ -338,7 +338,8 @@ hipError_t ln_bwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t 
 constexpr int64_t kParamsMax = (int64_t)1 << 16, kParamValuesMax = (int64_t)1 << 33;
 size_t grad_norm_ws(const haste_param_t *p, int64_t n);
 hipError_t grad_norm(const haste_param_t *p, int64_t n, float max_norm, float *out, void *ws, hipStream_t s);
-int64_t adamw_repeated(const haste_param_t *p, int64_t n);   // a tensor that names an updated array again, or -1
+// a tensor that names an updated array again, -1 where none does, -2 without host memory
+int64_t adamw_repeated(const haste_param_t *p, int64_t n);
 hipError_t adamw(const haste_param_t *p, int64_t n, const haste_adamw_opts_t &opt, hipStream_t s);
 // group-shared rewiring (Alg. 3); n_prune >= 1
 bool rewire_supported(const TailArgs &a);
