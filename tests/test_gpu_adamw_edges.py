@@ -43,3 +43,40 @@ def test_new_gradients_every_step(hs, bits):
         assert all(torch.equal(x, y) for x, y in zip(a.arrays().values(), b.arrays().values()))
     with pytest.raises(ValueError, match="is on cpu"):
         hs.set_grads(a.params, [torch.zeros(1000), None, None])
+
+
+def test_8bit_second_moments_settle_where_the_rounding_puts_them(hs):
+    """6000 steps of normally distributed gradients from v = sigma^2, sigma over 12 binades of each block.
+
+    A step moves the root by (c / 2) (g^2 - v) / r, c = 1 - beta2, and rounds it between neighbours D apart, with a
+    variance of |move| D less the move's square.  v takes that on and forgets c of it a step, so it settles above
+    sigma^2 by E|g^2 - v| / 2v times D / r, which is between 1/16 and 1/8 (no root is below 2^-13 of its block's
+    largest).  E|x^2 - 1| is 0.968 for a normal x, and 1.01 where v varies by 0.3 around 1.05; the squares take c / 4
+    E(x^2 - 1)^2 = 0.0005 off.  So 0.0298 .. 0.0632, and 0.003 for five standard errors of the mean.
+    The root's own deviation decays by 1 - c a step: a variance of 0.968 / 4 D / r, a standard deviation of 0.123 .. 0.174,
+    v's twice that and a little for its curvature: 0.24 .. 0.37."""
+    import torch
+    n = 1 << 18
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    sigma = torch.exp2(-12 * torch.rand(n, device="cuda", generator=gen))
+    sigma[::32] = 1.0
+    host = sigma.cpu().numpy()
+    q, s = ref._store(host, np.random.default_rng(12).integers(0, 65536, n), True)
+    got = {}
+    grad, W = torch.empty(n, device="cuda"), torch.zeros(n, device="cuda")
+    m8, v8, scale = torch.zeros(n, dtype=torch.uint8, device="cuda"), torch.from_numpy(q).cuda(), torch.zeros((n // 32, 2), dtype=torch.uint8, device="cuda")
+    scale[:, 1] = torch.from_numpy(s).cuda()
+    m32, v32 = torch.zeros(n, device="cuda"), sigma ** 2
+    lists = [hs.param_list([hs.param(W, grad, m8, v8, scale)]), hs.param_list([hs.param(W.clone(), grad, m32, v32)])]
+    opts = hs.adamw_opts(1e-3, seed=13)
+    for k in range(6000):
+        torch.randn(n, device="cuda", generator=gen, out=grad)
+        grad.mul_(sigma)
+        opts.step = 1000 + k
+        for p in lists:
+            hs.haste_adamw(p, opts)
+    r = v8.view(torch.float8_e4m3fn).double() * torch.exp2(scale[:, 1].double() - 127).repeat_interleave(32)
+    ratio = (r / sigma.double()) ** 2
+    bias = float(ratio.mean() / (v32.double() / sigma.double() ** 2).mean()) - 1
+    say(f"    v, 8 bits over 32: {bias:+.4f}, varies by {float(ratio.std()):.4f}")
+    assert 0.0268 < bias < 0.0662 and 0.24 < float(ratio.std()) < 0.37
