@@ -465,11 +465,14 @@ size_t haste_grad_norm_workspace_bytes(const haste_param_t *params, int64_t n_pa
  *       0.35 of itself around that.  Roots below 2^-13 of their block's largest have coarser spacings, and
  *       both grow by the same factor;
  *   a root above zero is stored as 2^-9 of the scale at least (else m would later be divided by eps alone);
- *   an infinity or a NaN becomes a NaN.
+ *   an infinity or a NaN becomes a NaN; so does the root of a v that is one (below).
  *   Draws: SplitMix64 as in haste_rewire, with key = out(0) of the stream seeded with seed + step.  Value i of
  *   tensor k of the list takes the 16 bits from bit 16 (i mod 4) on of out(k 2^40 + floor(i / 4)) of the stream
  *   seeded with key: d for m, 65535 - d for v.
  *
+ * A finite g whose (c2 g) g is beyond fp32 (|g| from 5.8e20 on at beta2 = 0.999) leaves an infinite v: in 32 bits the
+ * weight then moves by its decay alone, for good; in 8 bits v is stored as a NaN and the next step's weight is one.
+ * haste_grad_norm's factor keeps gradients far from there.
  * Where *grad_scale is an infinity or a NaN, the call changes nothing: a step whose gradients overflowed is
  * passed over.  lr_dev, step_dev and grad_scale are read when the kernels run, so that a captured graph
  * follows them.  With step_dev no more than the value is read: the caller counts.

@@ -80,3 +80,28 @@ def test_8bit_second_moments_settle_where_the_rounding_puts_them(hs):
     bias = float(ratio.mean() / (v32.double() / sigma.double() ** 2).mean()) - 1
     say(f"    v, 8 bits over 32: {bias:+.4f}, varies by {float(ratio.std()):.4f}")
     assert 0.0268 < bias < 0.0662 and 0.24 < float(ratio.std()) < 0.37
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_finite_gradients_whose_squares_overflow(hs, bits):
+    """(c2 g) g beyond fp32, from |g| = 5.8e20 at beta2 = 0.999 on: v is an infinity.  In 32 bits the weight moves by
+    its decay alone from then on; in 8 bits v is stored as a NaN, and the next step's weight is one.  Neither
+    reaches its neighbours, and just below the overflow nothing of the kind happens."""
+    import torch
+    t = Tensors(hs, [96], "f32", "f32", bits, decay=[0.0])
+    a = t.at[0]
+    t.grad[a + 40], t.grad[a + 90] = 6.0e20, 5.0e20
+    before = _step(hs, t, OPTS)
+    W = t.W[a:a + 96].clone()
+    assert bool(torch.isfinite(W).all()) and float(W[40]) == float(before["W"][a + 40])
+    if bits == 8:
+        assert int(t.v[a + 40]) == 0x7f and bool((t.m[a:a + 96] & 0x7f != 0x7f).all())
+    else:
+        assert math.isinf(float(t.v[a + 40])) and math.isfinite(float(t.v[a + 90]))
+    t.grad[a + 40] = t.grad[a + 90] = 1.0
+    for step in (8, 9, 10):
+        _step(hs, t, dict(OPTS, step=step))
+    now = t.W[a:a + 96]
+    others = torch.arange(96, device="cuda") != 40
+    assert bool(torch.isfinite(now[others]).all())
+    assert math.isnan(float(now[40])) if bits == 8 else float(now[40]) == float(W[40])
