@@ -285,10 +285,11 @@ __device__ __forceinline__ uint8_t store_e4m3(float x, uint32_t scale, uint32_t 
 
 // ---- the step of N values a lane --------------------------------------------------------------------
 // r = sqrt(v), correctly rounded (the 8-bit moments are rounded from it, and two implementations have to meet
-// the same value).  s = v y with y = 1 / sqrt(v) to one unit is off by a few units, and s + (v - s^2) y / 2, the
-// difference exact, rounds to the right one: compared with sqrtf for every value of two binades, so, within the
-// range below, for all.  Half of the instructions that sqrtf takes (58M bf16 weights and gradients with 8-bit
-// moments, where the vector ALUs are the bound: 132 us with it, 115 so).
+// the same value).  s = v y with y = 1 / sqrt(v) to one unit is off by a few units; one step of Newton's method with
+// the residual of a fused multiply-add, s + (v - s^2) y / 2, rounds to the right one.  Powers of four scale every step
+// exactly within the range below, so two binades stand for all: equal to sqrtf for every value of them (and of four
+// more).  Half of the instructions that sqrtf takes (58M bf16 weights and gradients with 8-bit moments, where the
+// vector ALUs are the bound: 132 us with it, 115 so).
 template <int N>
 __device__ __forceinline__ void roots(const float (&v)[N], float (&r)[N]) {
     uint32_t lo = __float_as_uint(v[0]), hi = lo;

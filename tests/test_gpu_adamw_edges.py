@@ -105,3 +105,35 @@ def test_finite_gradients_whose_squares_overflow(hs, bits):
     others = torch.arange(96, device="cuda") != 40
     assert bool(torch.isfinite(now[others]).all())
     assert math.isnan(float(now[40])) if bits == 8 else float(now[40]) == float(W[40])
+
+
+def _over_roots(hs, v, slow=None):
+    """1 / sqrt(v / 2) as the step forms it, for each v: m = 1 over the root in the update of a weight of zero.  slow:
+    the value of that number in each run of 256, a wave's, is one that sends its wave to the C library's sqrtf."""
+    import torch
+    v = v.clone()
+    if slow is not None:
+        v[slow::256] = 2.0 ** -99
+    W, grad, m = torch.zeros_like(v), torch.zeros_like(v), torch.full_like(v, 2.0)
+    hs.haste_adamw(hs.param_list([hs.param(W, grad, m, v)]), hs.adamw_opts(1.0, 0.5, 0.5, 1.2e-38, step=10000))
+    return W.neg_()
+
+
+@pytest.mark.parametrize("name,lo,count", [("all of [1, 4)", 2.0, 1 << 24), ("from 2^-90", 2.0 ** -89, 1 << 20),
+                                           ("from 2^126", 2.0 ** 127, 1 << 23)])
+def test_roots_are_those_of_sqrtf(hs, name, lo, count):
+    """Every fp32 value of two binades, the lowest ones of the range that the short way takes, and the largest ones that
+    half of a finite v can be: the same bits as from sqrtf, which rounds correctly.  A root that were one unit off
+    would show in its reciprocal always up to root 1.41 and every other time up to 2."""
+    import torch
+    start = int(np.float32(lo).view(np.int32))
+    v = torch.arange(start, start + count, dtype=torch.int32, device="cuda").view(torch.float32)
+    short = _over_roots(hs, v)
+    assert bool(torch.isfinite(v).all()) and int(v.numel()) % 256 == 0
+    for slow in (0, 1):
+        same = short.view(torch.int32) == _over_roots(hs, v, slow).view(torch.int32)
+        same[slow::256] = True
+        assert bool(same.all()), f"{int((~same).sum())} of {count}, the first for v = {float(v[~same][0]) / 2!r}"
+    # and what they are: the reciprocal is the hardware's, to one unit
+    want = 1 / (v.double() / 2).sqrt()
+    assert float(((short.double() - want).abs() / want).max()) <= 2.5 * 2.0 ** -23
