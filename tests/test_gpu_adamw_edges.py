@@ -137,3 +137,32 @@ def test_roots_are_those_of_sqrtf(hs, name, lo, count):
     # and what they are: the reciprocal is the hardware's, to one unit
     want = 1 / (v.double() / 2).sqrt()
     assert float(((short.double() - want).abs() / want).max()) <= 2.5 * 2.0 ** -23
+
+
+# lists of up to 2^22 values and of more take chunks of 4096 and of 16384 values; a round of loads takes 4096 fp32 or 8192 bf16
+@pytest.mark.parametrize("sizes", [[4194305, 16383, 8191, 8193], [16384 + 4096 + 8, 4 << 20, 7, 2047, 12289],
+                                   [4095, 4096, 4097, 8, 9, 7, 1], [2048, 2049, 2055, 2056, 1023, 6150, 3, 4104]])
+@pytest.mark.parametrize("dt", ["f32", "bf16", "both"])
+def test_norm_counts_every_value_once(hs, sizes, dt):
+    """Random values to rounding, and ones at a few hundred places, the ends of chunks, rounds and loads among them: one
+    that were left out or read twice would move the norm by a thousandth."""
+    import torch
+    kinds = {"f32": [torch.float32], "bf16": [torch.bfloat16], "both": [torch.float32, torch.bfloat16]}[dt]
+    gen = torch.Generator(device="cuda").manual_seed(len(sizes))
+    grads = [torch.randn(n, device="cuda", generator=gen).to(kinds[k % len(kinds)]) for k, n in enumerate(sizes)]
+    want = math.sqrt(sum(float((g.double() ** 2).sum()) for g in grads))
+    norm, factor = _norm(hs, grads, 1.0)
+    assert abs(norm - want) <= 1.01 * U * want and abs(factor * want - 1) <= 1.01 * U
+    rng = np.random.default_rng(sum(sizes))
+    edges = [e + j for e in range(0, max(sizes) + 1, 1024) for j in (-8, -5, -4, -1, 0, 3, 4, 7)]
+    for _ in range(4):
+        total = 0
+        for g, n in zip(grads, sizes):
+            at = [int(x) for x in rng.integers(0, n, 40)] + [0, n - 1, max(0, n - 4), max(0, n - 9), n // 8 * 8 - 1, n // 4 * 4 - 1]
+            at += [int(x) for x in rng.choice(edges, 60)]
+            at = sorted({p for p in at if 0 <= p < n})
+            g.zero_()
+            g[torch.tensor(at, device="cuda")] = 1.0
+            total += len(at)
+        norm, _ = _norm(hs, grads, math.inf)
+        assert norm == float(np.float32(math.sqrt(total))), (norm ** 2, total)
