@@ -166,3 +166,36 @@ def test_norm_counts_every_value_once(hs, sizes, dt):
             total += len(at)
         norm, _ = _norm(hs, grads, math.inf)
         assert norm == float(np.float32(math.sqrt(total))), (norm ** 2, total)
+
+
+KINDS = [("f32", "f32", 32, False), ("bf16", "f32", 32, True), ("bf16", "bf16", 32, False), ("bf16", "bf16", 8, False),
+         ("f32", "f32", 8, False), ("bf16", "f32", 8, True)]
+
+
+@pytest.mark.parametrize("w,g,bits,master", KINDS)
+def test_step_of_lists_beyond_two_million_values(hs, w, g, bits, master):
+    """Lists of more than 2^21 values a launch take whole chunks of 1024 values a workgroup, a lane's second run among
+    them, with the weights through the caches: ragged tensors, partial last blocks, against the plain form."""
+    t = Tensors(hs, [1_000_003, 1024, 1023, 31, 1_300_001, 1025 + 512, 33], w, g, bits, master)
+    for step in (1, 500):
+        o = dict(OPTS, step=step)
+        t.check(_step(hs, t, o), o)
+
+
+@pytest.mark.parametrize("w,g,bits,master", KINDS)
+def test_the_same_bits_on_both_sides_of_a_chunks_size(hs, w, g, bits, master):
+    """2^21 values a launch are the last in chunks of 512, one value more makes them 1024: the tensors in front come out
+    the same."""
+    import torch
+    n = 1 << 21
+    front = [5000, 2048 + 512 + 33, 1]
+    got = []
+    for rest in (n - sum(front), n - sum(front) + 1):
+        t = Tensors(hs, front, w, g, bits, master, edge=True)
+        last = Tensors(hs, [rest], "bf16", "bf16", 8, seed=1)
+        hs.haste_adamw(hs.param_list([*t.params, last.params[0]]), hs.adamw_opts(**OPTS))
+        torch.cuda.synchronize()
+        got.append(t.snapshot())
+    assert all(torch.equal(got[0][k], got[1][k]) for k in got[0])
+    before = Tensors(hs, front, w, g, bits, master, edge=True)
+    t.check(before.snapshot(), OPTS)
