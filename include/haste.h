@@ -410,8 +410,8 @@ int haste_layer_norm_fwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, i
  * H, ldh, weight, mean and rstd as in the forward call.  dH may be dX where type and stride are the same (it
  * must not overlap H or dX in any other way), and NULL to skip it; dweight[F] and dbias[F] fp32, each NULL to skip
  * it; beta is 0 (overwrite) or 1 (accumulate).
- * Sums are fp32; those over rows are formed in parts, in ws, and added in a fixed order (up to 512 rows in another
- * one where dH is dX).
+ * Sums are fp32; those over rows are formed in parts, in ws, and added in a fixed order (of few rows, up to 512, in
+ * another one where dH is dX).
  * ws: haste_layer_norm_workspace_bytes(B, F) bytes, where dweight or dbias is asked for.
  */
 int haste_layer_norm_bwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t ldh,

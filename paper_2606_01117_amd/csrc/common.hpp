@@ -331,6 +331,7 @@ hipError_t ln_fwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t 
                   const float *bias, float eps, int32_t dtype_x, void *X, int64_t ldx, float *mean, float *rstd,
                   hipStream_t s);
 size_t ln_bwd_ws(int64_t B, int64_t F);
+bool ln_bwd_few(int64_t B, int64_t F, int32_t dtype_h);   // the backward pass in one launch
 hipError_t ln_bwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t ldh, const float *weight,
                   const float *mean, const float *rstd, int32_t dtype_dx, const void *dX, int64_t lddx, void *dH,
                   int64_t lddh, float *dweight, float *dbias, int beta, void *ws, hipStream_t s);

@@ -567,8 +567,6 @@ BwdShape bwd_shape(int64_t B, int64_t F, int32_t dtype_h) {
     const int64_t want = haste::cdiv(B, threads / team);
     return {team, threads, want < 256 ? want : 256};
 }
-// Rows whose column sums a second pass over them, from the caches, forms as fast as partial sums would be added.
-constexpr int64_t kFewRows = 512;
 
 int64_t wide_parts(int64_t B) {
     const int64_t n = haste::cdiv(B, 64);
@@ -612,6 +610,18 @@ hipError_t ln_fwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t 
     return hipGetLastError();
 }
 
+// Rows whose column sums a second pass over them forms, in the same launch, as fast as a second launch would add partial
+// sums.  A workgroup of that pass takes eight columns, so it fetches lines that its neighbours fetch too, and of wide
+// rows' teams it leaves threads without a row: it is as good up to 1.3M to 2.1M values, by the team's threads.  (us in one
+// launch and in two, bf16 rows unless noted: 512 x 768 5.3 and 6.4; 512 x 2048 8.1 and 9.0, x 4096 15.7 and 12.2, x 8192
+// 30.1 and 18.8; 300 x 5000 11.1 and 14.2, 400 x 5000 14.1 and 14.3, 512 x 6144 20.1 and 16.0; fp32 200 x 5000 12.4 and
+// 13.5, 400 x 5000 17.4 and 15.5.  Below that the second launch costs the host 2.6: 64 x 8192 10.3 and 12.0 with it.)
+bool ln_bwd_few(int64_t B, int64_t F, int32_t dtype_h) {
+    if (B > 512 || !held(F)) return false;
+    const int threads = bwd_shape(B, F, dtype_h).threads;
+    return B * F <= (int64_t)(threads == 256 ? 8 : threads == 512 ? 6 : 5) << 18;
+}
+
 size_t ln_bwd_ws(int64_t B, int64_t F) {
     int64_t parts = wide_parts(B);
     if (held(F)) {
@@ -628,7 +638,7 @@ hipError_t ln_bwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t 
     const bool wg = dweight || dbias;
     const BwdShape n = held(F) ? bwd_shape(B, F, dtype_h) : BwdShape{};
     const int64_t parts = !held(F) ? wide_parts(B) : n.blocks;
-    const bool few = wg && B <= kFewRows && held(F) && dH != dX;
+    const bool few = wg && dH != dX && ln_bwd_few(B, F, dtype_h);
     with_type(dtype_h, [&](auto th) {
         with_type(dtype_dx, [&](auto td) {
             typedef decltype(th) TH;
