@@ -518,38 +518,53 @@ constexpr int kMaxRowBlocks = 65536;   // workgroups of the kernels for them; mo
 // The team that holds a row in few registers a thread, forward and backward (which adds up terms in registers too).
 constexpr int fwd_team(int64_t F) { return F <= 256 ? 16 : F <= 1024 ? 64 : F <= 4096 ? 256 : 1024; }
 constexpr int bwd_team(int64_t F) { return F <= 256 ? 16 : F <= 1024 ? 64 : F <= 2048 ? 256 : F <= 4096 ? 512 : 1024; }
-int64_t runs_of(int64_t F, int team) { return haste::cdiv(F, 4 * team); }
+constexpr int64_t runs_of(int64_t F, int team) { return (F + 4 * team - 1) / (4 * team); }
 
 // Where no more than three quarters of its runs were filled, a smaller team of up to six runs a thread takes bf16 rows
 // (39024 x 1025 bf16: forward 56 us and 37, backward 90 and 58; 8000 x 5000: 44 and 34, 69 and 50).  Rows of fp32 alone
 // are bound by memory with the runs half empty too, and slower in more registers (31250 x 1280: forward 58 and 61,
 // backward, where H's type decides, 91 and 100).
-int pick_team(int64_t F, int team, bool bf16) {
+constexpr int pick_team(int64_t F, int team, bool bf16) {
     const int small = team == 1024 || team == 512 ? 256 : team == 256 ? 64 : 16;
     return bf16 && team > 16 && 4 * F <= 3 * (4 * team * runs_of(F, team)) && runs_of(F, small) <= 6 ? small : team;
 }
 
-// f(team, runs of four values a thread), both as constants
-template <int LEAST, int MOST, typename F>
-void with_runs(int64_t n, F &&f) {
-    if constexpr (LEAST < MOST)
-        if (n > LEAST) return with_runs<LEAST + 1, MOST>(n, f);
-    f(std::integral_constant<int, LEAST>{});
+// The teams of both passes: bf16 as pick_team takes it.
+template <bool BF16>
+struct Forward {
+    static constexpr int team(int64_t F) { return pick_team(F, fwd_team(F), BF16); }
+};
+template <bool BF16>
+struct Backward {
+    static constexpr int team(int64_t F) { return pick_team(F, bwd_team(F), BF16); }
+};
+
+// a width that a pass gives to this team in this many runs: kernels are built for these alone
+template <typename PASS>
+constexpr bool taken(int team, int runs) {
+    for (int64_t F = 4 * team * (runs - 1) + 1; F <= 4 * team * runs && F <= kWideF; ++F)
+        if (F >= 4 && PASS::team(F) == team) return true;
+    return false;
 }
-template <typename F>
-void with_team(int team, int64_t width, F &&f) {
-    auto go = [&](auto t, auto least, auto most) {
-        with_runs<least, most>(runs_of(width, t), [&](auto nc) { f(t, nc); });
-    };
-    typedef std::integral_constant<int, 1> one;
-    typedef std::integral_constant<int, 2> two;
-    typedef std::integral_constant<int, 6> six;
+
+// f(team, runs of four values a thread), both as constants
+template <typename PASS, int TEAM, int RUNS, typename F>
+void with_runs(int64_t n, F &&f) {
+    if constexpr (RUNS <= 6) {
+        if (n != RUNS) return with_runs<PASS, TEAM, RUNS + 1>(n, f);
+        if constexpr (taken<PASS>(TEAM, RUNS)) f(std::integral_constant<int, TEAM>{}, std::integral_constant<int, RUNS>{});
+    }
+}
+template <typename PASS, typename F>
+void with_team(int64_t width, F &&f) {
+    const int team = PASS::team(width);
+    const int64_t n = runs_of(width, team);
     switch (team) {
-    case 16: return go(std::integral_constant<int, 16>{}, one{}, six{});
-    case 64: return go(std::integral_constant<int, 64>{}, two{}, six{});
-    case 256: return go(std::integral_constant<int, 256>{}, two{}, six{});
-    case 512: return go(std::integral_constant<int, 512>{}, two{}, two{});
-    default: return go(std::integral_constant<int, 1024>{}, two{}, std::integral_constant<int, 4>{});
+    case 16: return with_runs<PASS, 16, 1>(n, f);
+    case 64: return with_runs<PASS, 64, 1>(n, f);
+    case 256: return with_runs<PASS, 256, 1>(n, f);
+    case 512: return with_runs<PASS, 512, 1>(n, f);
+    default: return with_runs<PASS, 1024, 1>(n, f);
     }
 }
 
@@ -561,7 +576,8 @@ struct BwdShape {
     int64_t blocks;
 };
 BwdShape bwd_shape(int64_t B, int64_t F, int32_t dtype_h) {
-    const int team = pick_team(F, bwd_team(F), dtype_h == HASTE_DTYPE_BF16), most = bwd_threads((int)runs_of(F, team));
+    const int team = dtype_h == HASTE_DTYPE_BF16 ? Backward<true>::team(F) : Backward<false>::team(F);
+    const int most = bwd_threads((int)runs_of(F, team));
     int threads = team > 256 ? team : 256;
     while (threads < most && B > (int64_t)256 * 4 * (threads / team)) threads *= 2;
     const int64_t want = haste::cdiv(B, threads / team);
@@ -596,8 +612,7 @@ hipError_t ln_fwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t 
                                    dim3(kThreads), 0, s, B, F, (const TH *)H, ldh, weight, bias, eps, (TX *)X, ldx, mean, rstd);
                 return;
             }
-            const bool bf16 = dtype_h == HASTE_DTYPE_BF16 || dtype_x == HASTE_DTYPE_BF16;
-            with_team(pick_team(F, fwd_team(F), bf16), F, [&](auto team, auto nc) {
+            with_team<Forward<sizeof(TH) == 2 || sizeof(TX) == 2>>(F, [&](auto team, auto nc) {
                 // 16 waves a CU, which are all there at once, and 32 of teams that wait for each other (65536 x 768
                 // bf16 38.9 us with 16, 40.2 with 32; 8192 x 8192 63.7 and 51.8)
                 const int threads = team > 256 ? (int)team : 256;
@@ -660,7 +675,7 @@ hipError_t ln_bwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t 
             };
             const bool stream = whole(H, ldh, sizeof(TH)) && whole(dX, lddx, sizeof(TD));
             const Bwd<TH, TD> a = {B, (int)F, (const TH *)H, ldh, weight, mean, rstd, (const TD *)dX, lddx, (TH *)dH, lddh};
-            with_team(n.team, F, [&](auto team, auto nc) {
+            with_team<Backward<sizeof(TH) == 2>>(F, [&](auto team, auto nc) {
                 const int teams = n.threads / team;
                 const size_t lds = wg && teams > 1 ? (size_t)teams * cdiv(F, 4) * 16 : 0;
                 if (few) {

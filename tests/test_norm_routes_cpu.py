@@ -26,3 +26,36 @@ def test_few_rows_go_in_one_launch_where_that_is_faster(B, F, dtype, one, us):
     fn.restype, fn.argtypes = ctypes.c_bool, [ctypes.c_int64, ctypes.c_int64, ctypes.c_int32]
     assert fn(B, F, dtype) == one
     assert us is None or one == (us[0] < us[1])
+
+
+def _teams(F, backward, bf16):
+    """The team that takes a row, and its runs of four values a thread."""
+    runs = lambda team: -(-F // (4 * team))
+    limits = ((256, 16), (1024, 64), (2048, 256), (4096, 512)) if backward else ((256, 16), (1024, 64), (4096, 256))
+    team = next((t for most, t in limits if F <= most), 1024)
+    small = {1024: 256, 512: 256, 256: 64, 64: 16}.get(team)
+    if bf16 and small and 4 * F <= 3 * 4 * team * runs(team) and runs(small) <= 6:
+        team = small
+    return team, runs(team)
+
+
+def test_no_kernel_is_built_that_no_width_takes():
+    import re
+    import subprocess
+
+    from paper_2606_01117_amd import LIB_PATH
+    out = subprocess.run(["nm", "-C", LIB_PATH], capture_output=True, text=True, check=True).stdout
+    built = set(re.findall(r"__device_stub__(k_ln_\w+)<(.*?)>\(", out))
+    types = {"float": False, "__hip_bfloat16": True, "unsigned short": True}
+    names = {n for _, args in built for n in args.split(", ")[:2]}
+    assert names <= set(types), names
+    want = set()
+    for F in range(4, 16385):
+        for a in names:
+            for b in names:
+                fwd, bwd = _teams(F, False, types[a] or types[b]), _teams(F, True, types[a])
+                want.add(("k_ln_fwd", f"{a}, {b}, {fwd[0]}, {fwd[1]}"))
+                want.add(("k_ln_bwd_few", f"{a}, {b}, {bwd[0]}, {bwd[1]}"))
+                want |= {("k_ln_bwd", f"{a}, {b}, {bwd[0]}, {bwd[1]}, {stream}") for stream in ("false", "true")}
+    held = {k for k in built if k[0] in ("k_ln_fwd", "k_ln_bwd", "k_ln_bwd_few")}
+    assert held == want, (sorted(held - want)[:5], sorted(want - held)[:5])
