@@ -30,3 +30,10 @@ def _both(hs, B, F, h, x):
 @pytest.mark.parametrize("h,x", [("bf16", "f32"), ("f32", "f32"), ("f32", "bf16")])
 def test_few_rows(hs, B, F, h, x):
     _both(hs, B, F, h, x)
+
+
+# 64 KB of LDS: 64 teams of a row of up to 256 values, 16 of a row of up to 1024
+@pytest.mark.parametrize("B,F", [(32769, 256), (40001, 193), (8193, 1024), (9001, 1001), (32768, 256), (8192, 1024)])
+@pytest.mark.parametrize("h,x", [("bf16", "f32"), ("f32", "bf16")])
+def test_workgroups_that_add_up_the_most_teams(hs, B, F, h, x):
+    _both(hs, B, F, h, x)
