@@ -398,13 +398,27 @@ def haste_layer_norm_bwd(B, F, dtype_h, H, weight, mean, rstd, dtype_dx, dX, dH=
                                     _stream(stream)))
 
 
+_codes = {}
+
+
 def _dtype_of(t, name) -> int:
-    torch = _torch()
-    if t.dtype is torch.float32:
-        return HASTE_DTYPE_F32
-    if t.dtype is torch.bfloat16:
-        return HASTE_DTYPE_BF16
-    raise ValueError(f"{name} must be torch.float32 or torch.bfloat16, got {t.dtype}")
+    if not _codes:
+        _codes.update({_torch().float32: HASTE_DTYPE_F32, _torch().bfloat16: HASTE_DTYPE_BF16})
+    code = _codes.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be torch.float32 or torch.bfloat16, got {t.dtype}")
+    return code
+
+
+_byte_types_of = []
+
+
+def _byte_types():
+    """The types of 8-bit moments and of their scales: bytes, or what they stand for."""
+    if not _byte_types_of:
+        torch = _torch()
+        _byte_types_of.extend(({torch.uint8, torch.int8, torch.float8_e4m3fn}, {torch.uint8, torch.int8, torch.float8_e8m0fnu}))
+    return _byte_types_of
 
 
 def param(W=None, grad=None, m=None, v=None, scale=None, W32=None, lr_scale=1.0, weight_decay=0.0) -> haste_param_t:
@@ -431,10 +445,10 @@ def param(W=None, grad=None, m=None, v=None, scale=None, W32=None, lr_scale=1.0,
     if m is not None and v is not None:
         if m.element_size() == 1 and v.element_size() == 1:
             bits = 8
-            for t, name in ((m, "m"), (v, "v")):
-                if t.dtype not in (_torch().uint8, _torch().int8, _torch().float8_e4m3fn):    # bytes, or what they are
-                    raise ValueError(f"8-bit {name} must be uint8 or float8_e4m3fn, got {t.dtype}")
-            if scale is None or scale.dtype not in (_torch().uint8, _torch().int8, _torch().float8_e8m0fnu):
+            moments, exponents = _byte_types()
+            if m.dtype not in moments or v.dtype not in moments:
+                raise ValueError(f"8-bit moments must be uint8 or float8_e4m3fn, got {m.dtype} and {v.dtype}")
+            if scale is None or scale.dtype not in exponents:
                 raise ValueError(f"8-bit moments of {n} values need scale, uint8 [{(n + 31) // 32}, 2]")
         elif _dtype_of(m, "m") != HASTE_DTYPE_F32 or _dtype_of(v, "v") != HASTE_DTYPE_F32:
             raise ValueError("m and v must both be torch.float32, or both of one byte a value")
@@ -478,12 +492,14 @@ def param_list(params):
     it at new gradients).  Entries may be taken out of one list and put into another, or replaced in place."""
     params = list(params)
     n = len(params)
+    devices = {getattr(p, "device", None) for p in params} - {None}
+    if len(devices) > 1:
+        raise ValueError(f"the tensors of a list must be on one GPU, not on {sorted(devices)}")
     if n not in _list_types:
         _list_types[n] = type("param_list", (_Entries, haste_param_t * n), {})
-    array = _list_types[n]()
-    array.keep, array.device = [None] * n, None
-    for k, p in enumerate(params):
-        array[k] = p
+    array = _list_types[n].from_buffer((haste_param_t * n)(*params)) if n else _list_types[n]()
+    array.keep = [getattr(p, "keep", None) for p in params]
+    array.device = devices.pop() if devices else None
     return array
 
 
@@ -512,11 +528,16 @@ def set_grads(params, grads):
     params.device = device
 
 
-def _still_here(what, name):
-    """Tensors that a list or options hold must be on the GPU that is current at the call, too."""
-    device = getattr(what, "device", None)
-    if device is not None and device != _torch().cuda.current_device():
-        raise ValueError(f"{name} are on cuda:{device}, not on the current device cuda:{_torch().cuda.current_device()}")
+def _still_here(params, opts=None):
+    """Tensors that a list and options hold must be on the GPU that is current at the call, too."""
+    a, b = getattr(params, "device", None), getattr(opts, "device", None)
+    if a is None and b is None:
+        return
+    now = _torch().cuda.current_device()
+    if (a is None or a == now) and (b is None or b == now):
+        return
+    device, whose = (b, "options'") if a is None or a == now else (a, "list's")
+    raise ValueError(f"the {whose} tensors are on cuda:{device}, not on the current device cuda:{now}")
 
 
 def adamw_opts(lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, seed=0, lr_dev=None, step_dev=None,
@@ -544,7 +565,7 @@ def haste_grad_norm_workspace_bytes(params) -> int:
 
 def haste_grad_norm(params, max_norm, out, ws=None, stream=None):
     """params: a param_list; out: two fp32 values on the GPU, the norm and the factor that clips it to max_norm."""
-    _still_here(params, "the list's tensors")
+    _still_here(params)
     p, n = _ws(ws)
     _check(lib.haste_grad_norm(params, len(params), max_norm, _vec(out, 2, "out", _here(out, "out")), p, n,
                                _stream(stream)))
@@ -552,8 +573,7 @@ def haste_grad_norm(params, max_norm, out, ws=None, stream=None):
 
 def haste_adamw(params, opts, stream=None):
     """One AdamW step over a param_list, in place."""
-    _still_here(params, "the list's tensors")
-    _still_here(opts, "the options' tensors")
+    _still_here(params, opts)
     _check(lib.haste_adamw(params, len(params), ctypes.byref(opts), _stream(stream)))
 
 
