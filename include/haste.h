@@ -393,7 +393,8 @@ int haste_head_bwd(int64_t B, int64_t F_s, int64_t H, int32_t dtype, const void 
  * (NULL): what haste_layer_norm_bwd takes.  X may be H where type and stride are the same.
  * X must not overlap H in any other way.
  * Arithmetic: fp32, the squares around the row's mean; a bf16 X is rounded once.  An infinity or a NaN
- * makes its own row NaN.  eps >= 0; at 0 a row of equal values is NaN.  1 <= F <= 2^24; B < 2^31, B == 0
+ * makes its own row NaN, and so does a sum beyond fp32; differences from the mean whose squares are beyond it (2^64 and
+ * more) make rstd 0 and X the bias.  eps >= 0; at 0 a row of equal values is NaN.  1 <= F <= 2^24; B < 2^31, B == 0
  * launches nothing.
  */
 int haste_layer_norm_fwd(int64_t B, int64_t F, int32_t dtype_h, const void *H, int64_t ldh,

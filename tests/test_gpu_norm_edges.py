@@ -37,3 +37,22 @@ def test_few_rows(hs, B, F, h, x):
 @pytest.mark.parametrize("h,x", [("bf16", "f32"), ("f32", "bf16")])
 def test_workgroups_that_add_up_the_most_teams(hs, B, F, h, x):
     _both(hs, B, F, h, x)
+
+
+@pytest.mark.parametrize("F", [3, 64, 768, 3000, 9001, 16385])
+def test_rows_beyond_the_range_of_their_squares(hs, F):
+    """Differences from the mean of 2^64 and more have squares beyond fp32: rstd is 0 and X the bias.  A sum beyond fp32
+    makes its row NaN.  Neither reaches another row, nor dH of theirs."""
+    import torch
+    c = Case(4, F, "f32", "f32")
+    c.H[1] = 0.0
+    c.H[1, 0] = 2.0 ** 100                       # its sum, mean and difference are exact powers or near
+    c.H[2] = 3e38
+    X, mean, rstd = c.forward(hs)
+    assert float(rstd[1]) == 0.0 and torch.equal(X[1], c.b)
+    assert bool(torch.isnan(X[2]).all())
+    out, mu, rs, tx, tm, tr = c.reference()
+    for k in (0, 3):
+        assert (abs(X[k].cpu().numpy() - out[k]) <= tx[k]).all()
+    dH = c.backward(hs, mean, rstd, dw=None, db=None)[0]
+    assert bool((dH[1] == 0).all()) and bool(torch.isfinite(dH[[0, 3]]).all())
