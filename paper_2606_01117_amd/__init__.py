@@ -165,13 +165,14 @@ def _torch():
     return _torch_module
 
 
-def _stream(stream) -> Optional[int]:
+def _stream(stream, device=None) -> Optional[int]:
+    """The handle of a stream; None is the current one (of the current device, if the caller knows it)."""
     if stream is None:
         torch = _torch()
         # the current stream's handle; without this entry, through a Stream object, which takes ten times as long
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         if raw is not None:
-            return raw(torch.cuda.current_device())
+            return raw(torch.cuda.current_device() if device is None else device)
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
@@ -379,7 +380,7 @@ def haste_layer_norm_fwd(B, F, dtype_h, H, weight, bias, eps, dtype_x, X, mean=N
         _elsewhere(X, "X")
     _check(lib.haste_layer_norm_fwd(B, F, dtype_h, h, ldh, _vec(weight, F, "weight", on), _vec(bias, F, "bias", on), eps,
                                     dtype_x, x, ldx, _vec(mean, B, "mean", on), _vec(rstd, B, "rstd", on),
-                                    _stream(stream)))
+                                    _stream(stream, on)))
 
 
 def haste_layer_norm_bwd(B, F, dtype_h, H, weight, mean, rstd, dtype_dx, dX, dH=None, dweight=None, dbias=None, beta=0,
@@ -395,7 +396,7 @@ def haste_layer_norm_bwd(B, F, dtype_h, H, weight, mean, rstd, dtype_dx, dX, dH=
     _check(lib.haste_layer_norm_bwd(B, F, dtype_h, h, ldh, _vec(weight, F, "weight", on), _vec(mean, B, "mean", on),
                                     _vec(rstd, B, "rstd", on), dtype_dx, dx, lddx, dh, lddh,
                                     _vec(dweight, F, "dweight", on), _vec(dbias, F, "dbias", on), int(beta), p, n,
-                                    _stream(stream)))
+                                    _stream(stream, on)))
 
 
 _codes = {}
@@ -529,13 +530,13 @@ def set_grads(params, grads):
 
 
 def _still_here(params, opts=None):
-    """Tensors that a list and options hold must be on the GPU that is current at the call, too."""
+    """Tensors that a list and options hold must be on the GPU that is current at the call, too; that GPU, if they hold any."""
     a, b = getattr(params, "device", None), getattr(opts, "device", None)
     if a is None and b is None:
-        return
+        return None
     now = _torch().cuda.current_device()
     if (a is None or a == now) and (b is None or b == now):
-        return
+        return now
     device, whose = (b, "options'") if a is None or a == now else (a, "list's")
     raise ValueError(f"the {whose} tensors are on cuda:{device}, not on the current device cuda:{now}")
 
@@ -565,16 +566,16 @@ def haste_grad_norm_workspace_bytes(params) -> int:
 
 def haste_grad_norm(params, max_norm, out, ws=None, stream=None):
     """params: a param_list; out: two fp32 values on the GPU, the norm and the factor that clips it to max_norm."""
-    _still_here(params)
+    on = _still_here(params)
     p, n = _ws(ws)
     _check(lib.haste_grad_norm(params, len(params), max_norm, _vec(out, 2, "out", _here(out, "out")), p, n,
-                               _stream(stream)))
+                               _stream(stream, on)))
 
 
 def haste_adamw(params, opts, stream=None):
     """One AdamW step over a param_list, in place."""
-    _still_here(params, opts)
-    _check(lib.haste_adamw(params, len(params), ctypes.byref(opts), _stream(stream)))
+    on = _still_here(params, opts)
+    _check(lib.haste_adamw(params, len(params), ctypes.byref(opts), _stream(stream, on)))
 
 
 def haste_validate_idx(desc, idx, n_bad_rows, stream=None):

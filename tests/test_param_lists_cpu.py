@@ -172,20 +172,23 @@ def test_options_and_lists_made_on_another_device_are_refused(hs, on_host, monke
 
 
 def test_the_check_for_arrays_named_twice_takes_its_time_by_tensor(hs):
-    """Lists of 2048 and of 65536 tensors, the last one of which names the weights of the one before: no more than six
-    times the time a tensor (a search for each of them in steps of 512 took 21 times, 31 ms in all)."""
+    """Lists of 2048 and of 65536 tensors, the last one of which names the weights of the one before.  Going through the
+    list once for every 512 tensors looks at 2 and at 64 of those runs on average for each tensor, 32 times as much
+    (measured 21 times the time); looking each up once, at one (2 to 3 times, for the larger table).  The processor's time of
+    this thread, the least of many."""
     import ctypes
     import time
-    took = {}
+    lists, took = {}, {}
     for n in (2048, 65536):
-        params = (hs.haste_param_t * n)()
+        params = lists[n] = (hs.haste_param_t * n)()
         for j, p in enumerate(params):
             p.W, p.grad, p.m, p.v, p.n, p.state_bits = *((8 * j + i) << 20 for i in (1, 2, 3, 4)), 64, 32
         params[n - 1].v = params[n - 2].W
-        opts, took[n] = hs.adamw_opts(1e-3), 1e9
-        for _ in range(7):
-            start = time.perf_counter()
+    opts = hs.adamw_opts(1e-3)
+    for _ in range(15):
+        for n, params in lists.items():
+            start = time.thread_time_ns()
             assert hs.lib.haste_adamw(params, n, ctypes.byref(opts), None) == 1
-            took[n] = min(took[n], (time.perf_counter() - start) / n)
-        assert f"tensor {n - 1}:" in hs.haste_last_error() and "twice" in hs.haste_last_error()
-    assert took[65536] < 6 * took[2048], took
+            took[n] = min(took.get(n, 1e12), (time.thread_time_ns() - start) / n)
+            assert f"tensor {n - 1}:" in hs.haste_last_error() and "twice" in hs.haste_last_error()
+    assert took[65536] < 10 * took[2048], took
