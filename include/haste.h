@@ -463,8 +463,8 @@ size_t haste_grad_norm_workspace_bytes(const haste_param_t *params, int64_t n_pa
  *       on r's variance.  Where it moves by little a step (1 - beta2 well below 1/16), it settles above the
  *       32-bit moment by half of the mean of |grad^2 - v| / v times r's spacing over r, 1/16 to 1/8: by 3 to
  *       6.5 % under gradients of a normal distribution, by 13 % at most under any, and it varies by 0.25 to
- *       0.35 of itself around that.  Roots below 2^-13 of their block's largest have coarser spacings, and
- *       both grow by the same factor;
+ *       0.35 of itself around that.  Roots below 2^-13 of their block's largest have coarser spacings, by
+ *       whose factor the first grows, and by the factor's root the second;
  *   a root above zero is stored as 2^-9 of the scale at least (else m would later be divided by eps alone);
  *   an infinity or a NaN becomes a NaN; so does the root of a v that is one (below).
  *   Draws: SplitMix64 as in haste_rewire, with key = out(0) of the stream seeded with seed + step.  Value i of

@@ -507,7 +507,8 @@ def param_list(params):
 def set_grads(params, grads):
     """Points a param_list at new gradients, in the order of its entries: contiguous, fp32 or bf16, of the entries' sizes,
     on the list's GPU; None leaves an entry's gradient as it is.  The list keeps the new tensors alive and no longer the
-    old ones; nothing is changed where one of them is refused.  A graph captured before holds the old addresses."""
+    old ones (which, as any tensor, must live on where a call on another stream still reads them); nothing is changed
+    where one of them is refused.  A graph captured before holds the old addresses."""
     grads = list(grads)
     if len(grads) != len(params):
         raise ValueError(f"{len(grads)} gradients for a list of {len(params)} tensors")

@@ -56,3 +56,50 @@ def test_rows_beyond_the_range_of_their_squares(hs, F):
         assert (abs(X[k].cpu().numpy() - out[k]) <= tx[k]).all()
     dH = c.backward(hs, mean, rstd, dw=None, db=None)[0]
     assert bool((dH[1] == 0).all()) and bool(torch.isfinite(dH[[0, 3]]).all())
+
+
+@pytest.mark.parametrize("h", ["bf16", "f32"])
+@pytest.mark.parametrize("B,F,rows", [(20001, 131, 1), (9001, 768, 1), (8999, 769, 2), (3000, 2050, 1), (2500, 4096, 1),
+                                      (700, 9001, 1), (600, 16000, 1), (3000, 20001, 1)])
+def test_in_place_over_many_rows(hs, h, B, F, rows):
+    """Teams of several rows, each asked for before the one in front of it is stored."""
+    import torch
+    c = Case(B, F, h, h, rows=rows)
+    X, mean, rstd = c.forward(hs)
+    few = c.backward(hs, mean, rstd)
+    d = c.dX.clone()
+    got = c.backward(hs, mean, rstd, dH=d, dX=d)
+    assert all(torch.equal(a, b) for a, b in zip(few, got))
+    between = c.store.clone()
+    c.forward(hs, X=c.H)
+    assert torch.equal(c.H, X)
+    c.H.copy_(between[:B * c.ld].view(B, c.ld)[:, :F])
+    assert torch.equal(c.store, between), "what lies between the rows"
+
+
+def test_two_graphs_share_a_workspace(hs):
+    """Backward passes of more rows than one launch takes, captured one by one over the same workspace and replayed in
+    turn, with eager calls over it in between."""
+    import torch
+    cases = [Case(2000, 768, "bf16", "f32"), Case(700, 1003, "f32", "bf16"), Case(9000, 100, "bf16", "bf16")]
+    stats = [c.stats() for c in cases]
+    ws = hs.workspace(max(hs.haste_layer_norm_workspace_bytes(c.B, c.F) for c in cases))
+    outs = [c.backward(hs, *s, ws=ws) for c, s in zip(cases, stats)]
+    graphs, side = [], torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for c, s, o in zip(cases, stats, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            c.backward(hs, *s, *o, ws=ws)
+    for _ in range(3):
+        for c in cases:
+            c.dX.normal_()
+        for g in (*graphs, graphs[0]):
+            g.replay()
+        torch.cuda.synchronize()
+        for c, s, o in zip(cases, stats, outs):
+            got = [t.clone() for t in o]
+            for t in o:
+                t.fill_(9.0)
+            c.backward(hs, *s, *o, ws=ws)
+            assert all(torch.equal(a, b) for a, b in zip(got, o))
