@@ -25,7 +25,7 @@ def _both(hs, B, F, h, x):
 
 
 # in one launch and in two
-@pytest.mark.parametrize("B,F", [(512, 3072), (512, 3073), (512, 4096), (512, 4097), (300, 7168), (180, 7168), (160, 8192),
+@pytest.mark.parametrize("B,F", [(512, 3040), (512, 3073), (512, 4096), (512, 4097), (300, 7168), (180, 7168), (160, 8192),
                                  (161, 8192), (17, 8192), (80, 16384), (130, 12289), (512, 16384), (513, 768), (512, 1)])
 @pytest.mark.parametrize("h,x", [("bf16", "f32"), ("f32", "f32"), ("f32", "bf16")])
 def test_few_rows(hs, B, F, h, x):
